@@ -45,6 +45,13 @@ extern "C" {
 #define HAQ_ACT_NONE 0
 #define HAQ_ACT_RELU 1
 
+#define HAQ_F16 0  /* 16-bit rows of the calls that take a dtype: binary16 */
+#define HAQ_BF16 1 /* bfloat16 */
+
+#define HAQ_CODES_NONE 0
+#define HAQ_CODES_I8 1   /* int8, one scale for each token */
+#define HAQ_CODES_E4M3 2 /* 8-bit floating point, one scale for 128 channels of a token */
+
 #define HAQ_LOC_DEVICE 0      /* expert weights live in HBM */
 #define HAQ_LOC_HOST_PINNED 1 /* expert weights live in pinned host memory and are streamed in */
 
@@ -163,6 +170,72 @@ int32_t haq_w8a8_linear_asym(const void* x_fp16, int64_t ldx, const float* s, co
                              int32_t act, void* y_fp16, int64_t ldy, int32_t* acc_dbg, uint8_t* q_dbg,
                              float* sx_dbg, int32_t* zp_dbg, void* workspace, size_t workspace_bytes,
                              void* stream);
+
+/* ------------------------------------------------------------------------
+ * The linear layer in 8-bit floating point with a scale for each block of 128
+ * channels, next to the int8 one: no smoothing vector, no calibration; an outlier
+ * channel costs precision in its own block only.  Codes are e4m3 (four exponent,
+ * three mantissa bits, largest 448, no infinities, NaN 0x7f).
+ *   weights: one scale for 128 x 128 (input x output channels), sw [ceil(K/128) x ceil(N/128)];
+ *   activations: one scale for 128 channels of a token.
+ * Of either block, a = largest magnitude (NaN apart): scale = a / 448, code = e4m3(v * (448 /
+ * a)), binary32, round half to even; a < 2^-100 gives scale 0 and codes 0.  A NaN has a NaN
+ * code; an infinity makes its block's scale infinite and its own code NaN: either way every
+ * output of the token (or of the 128 channels, in a weight) is NaN.
+ *   y[t][n] = round16(act(sum over blocks b of (sx[t][b] * sw[b][n/128]) * p_b)),
+ *   p_b = the sum over the block's channels of code products, formed by the matrix
+ * instruction: error below 2^-10 of the sum of the products' magnitudes (it sums each eight in
+ * whole steps of 2^-13 of the largest).  The sum
+ * over blocks is binary32, one fused multiply-add per block; its order goes by the kernel that
+ * the sizes choose, so two row counts may differ in the last bits (a call repeated does not).
+ * ReLU passes NaN on.
+ *
+ * x and y are binary16 or bfloat16 by dtype (HAQ_F16, HAQ_BF16; both the same), rows
+ * [T x K] and [T x N].  K % 16 == 0, K <= 65536, N % 16 == 0, T and N <= 2^24.  T == 0 is a
+ * no-op.  y must not overlap an input.
+ *
+ * haq_quant_weight_fp8 (offline): w fp32 [K x N] -> wq [K x N] codes, canonical layout,
+ *   and w_scale; to be packed with haq_pack_weight like int8 codes (the layout is of bytes).
+ * haq_quant_act_fp8_packed: codes of x in the packed activation layout (haq_packed_act_rows,
+ *   haq_packed_act_bytes) and block_scale [ceil(K/128)][R], R = haq_packed_act_rows(T) (size:
+ *   haq_act_scales_fp8_bytes).  Rows behind the last token are not written and count for nothing.
+ * haq_gemm_fp8_packed: the linear on such codes.  haq_fp8_linear: on 16-bit rows, codes and scales
+ *   in the workspace (256-byte aligned, haq_fp8_linear_workspace_bytes); results as of the two
+ *   calls but for the order of the sum over blocks.                                          */
+int32_t haq_quant_weight_fp8(const float* w, int32_t K, int32_t N, uint8_t* wq, float* w_scale, void* stream);
+size_t haq_act_scales_fp8_bytes(int32_t T, int32_t K);
+int32_t haq_quant_act_fp8_packed(const void* x, int64_t ldx, int32_t dtype, int32_t T, int32_t K, uint8_t* q_packed,
+                                 float* block_scale, void* stream);
+int32_t haq_gemm_fp8_packed(const uint8_t* q_packed, const float* block_scale, const uint8_t* w_packed,
+                            const float* w_scale, int32_t T, int32_t K, int32_t N, int32_t act, int32_t dtype, void* y,
+                            int64_t ldy, void* stream);
+size_t haq_fp8_linear_workspace_bytes(int32_t T, int32_t K, int32_t N);
+int32_t haq_fp8_linear(const void* x, int64_t ldx, int32_t dtype, const uint8_t* w_packed, const float* w_scale,
+                       int32_t T, int32_t K, int32_t N, int32_t act, void* y, int64_t ldy, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Root-mean-square norm with the residual's addition, and codes as output: what
+ * stands in front of a linear (or of the router and the experts) in a decoder layer.
+ *   h = round16(x + residual)  (h = x without one);
+ *   inv = binary32(1 / sqrt(mean_k h^2 + eps)), in binary64 up to that rounding;
+ *   v_k = (h_k * inv) * weight_k  (binary32, two roundings);  y = round16(v).
+ * codes:
+ *   HAQ_CODES_I8: a = max_k |v|, scale = a / 127, q = rne(v / scale): the operand of
+ *     haq_gemm_w8a8_packed.  For a smoothed layer pass weight_k / s_k.  a < 2^-100 gives scale 0,
+ *     codes 0; with an infinity or NaN in the row scale is not finite either, codes 0 (every output NaN).
+ *   HAQ_CODES_E4M3: as haq_quant_act_fp8_packed, on v: the operand of haq_gemm_fp8_packed.
+ * Codes are of v, not of y, so they carry one rounding fewer than y quantised afterwards.
+ *
+ * x, residual (or NULL), sum, y: 16-bit rows [T x K] of one dtype, row strides in elements (multiples
+ * of 8).  weight fp32 [K].  sum (optional, with a residual only): h, the residual stream of the
+ * next layer.  y optional if codes are asked for.  q_packed and scale (both or neither): the packed layout,
+ * haq_packed_act_bytes(T, K) bytes, and fp32 [T] or [ceil(K/128)][haq_packed_act_rows(T)]; rows behind the
+ * last token are not written.  sum and y may be x or residual themselves (same address and
+ * stride); no other overlap.  1e-30 <= eps <= 1e30, K % 16 == 0, K <= 65536, T <= 2^24.         */
+int32_t haq_rmsnorm_quant(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, double eps,
+                          int32_t dtype, int32_t T, int32_t K, void* sum, int64_t lds, void* y, int64_t ldy,
+                          int32_t codes, void* q_packed, float* scale, void* stream);
 
 /* ------------------------------------------------------------------------
  * Two chained smoothed W8A8 linears (a dense FFN block, e.g. OPT: fc1, ReLU, fc2):

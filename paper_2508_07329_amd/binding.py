@@ -29,10 +29,15 @@ __all__ = [
     "haq_inverse_cholesky_upper_f64", "haq_hessian_quant_weight",
     "haq_weight_colsum", "haq_linear_asym_workspace_bytes", "haq_w8a8_linear_asym",
     "haq_quantize_layer_workspace_bytes", "haq_quantize_layer",
+    "haq_quant_weight_fp8", "haq_act_scales_fp8_bytes", "haq_quant_act_fp8_packed", "haq_gemm_fp8_packed",
+    "haq_fp8_linear_workspace_bytes", "haq_fp8_linear", "haq_rmsnorm_quant",
+    "HAQ_F16", "HAQ_BF16", "HAQ_CODES_NONE", "HAQ_CODES_I8", "HAQ_CODES_E4M3",
 ]
 
 HAQ_ACT_NONE, HAQ_ACT_RELU = 0, 1
 HAQ_LOC_DEVICE, HAQ_LOC_HOST_PINNED = 0, 1
+HAQ_F16, HAQ_BF16 = 0, 1
+HAQ_CODES_NONE, HAQ_CODES_I8, HAQ_CODES_E4M3 = 0, 1, 2
 HAQ_DECISION_GPU_CACHED, HAQ_DECISION_TRANSFER, HAQ_DECISION_CPU = 0, 1, 2
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -54,6 +59,8 @@ EXPORTED_SYMBOLS = [
     "haq_inverse_cholesky_upper_f64", "haq_hessian_quant_weight",
     "haq_weight_colsum", "haq_linear_asym_workspace_bytes", "haq_w8a8_linear_asym",
     "haq_quantize_layer_workspace_bytes", "haq_quantize_layer",
+    "haq_quant_weight_fp8", "haq_act_scales_fp8_bytes", "haq_quant_act_fp8_packed", "haq_gemm_fp8_packed",
+    "haq_fp8_linear_workspace_bytes", "haq_fp8_linear", "haq_rmsnorm_quant",
 ]
 
 
@@ -85,7 +92,12 @@ _CALLS = {
     "haq_moe_w8a8_ffn": (_P, _P, _L, _P, _L, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P, _P, _Z, _P),
     "haq_moe_w8a8_ffn_static": (_P, _L, _P, _L, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P),
     "haq_moe_w8a8_ffn_asym": (_P, _L, _P, _L, _P, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P, _P, _Z, _P),
+    "haq_quant_act_fp8_packed": (_P, _L, _I, _I, _I, _P, _P, _P),
+    "haq_gemm_fp8_packed": (_P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P),
+    "haq_fp8_linear": (_P, _L, _I, _P, _P, _I, _I, _I, _I, _P, _L, _P, _Z, _P),
 }
+# ... and of one with a floating-point argument.
+_NORM_TYPES = (_P, _L, _P, _L, _P, C.c_double, _I, _I, _I, _P, _L, _P, _L, _I, _P, _P, _P)
 
 _lib = None
 
@@ -102,11 +114,13 @@ def lib() -> C.CDLL:
         for n in ("haq_packed_bytes", "haq_linear_workspace_bytes", "haq_moe_workspace_bytes", "haq_packed_act_bytes",
                   "haq_ffn_workspace_bytes", "haq_smoothing_search_workspace_bytes", "haq_hessian_quant_workspace_bytes",
                   "haq_inverse_cholesky_workspace_bytes", "haq_linear_asym_workspace_bytes",
-                  "haq_quantize_layer_workspace_bytes", "haq_moe_asym_workspace_bytes", "haq_linear_kn_workspace_bytes"):
+                  "haq_quantize_layer_workspace_bytes", "haq_moe_asym_workspace_bytes", "haq_linear_kn_workspace_bytes",
+                  "haq_act_scales_fp8_bytes", "haq_fp8_linear_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.haq_packed_act_rows.restype = C.c_int64
         for n, types in _CALLS.items():
             getattr(L, n).argtypes = types
+        L.haq_rmsnorm_quant.argtypes = _NORM_TYPES
         _lib = L
     return _lib
 
@@ -275,6 +289,154 @@ def haq_gemm_w8a8_packed(q_packed, row_scale, w_packed, w_scale, T: int, K: int,
     _check(lib().haq_gemm_w8a8_packed(_adr(q_packed), _adr(row_scale), _adr(w_packed), _adr(w_scale), T, K, N, act,
                                       _adr(y), y.stride(0), None, _stream_adr()))
     return y
+
+
+# ---- 8-bit floating point with block scales, and the norm in front of a linear ------------
+_DTYPES = {torch.float16: HAQ_F16, torch.bfloat16: HAQ_BF16}
+
+
+def _rows16(name, **tensors):
+    """The dtype number of 16-bit rows [T, K]; raises if they differ in shape or type, or live on another GPU than the current
+    one (whose stream the work goes to)."""
+    first = None
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        first = t if first is None else first
+        if t.dim() != 2 or t.dtype not in _DTYPES or t.dtype != first.dtype or t.shape != first.shape:
+            raise HaqError(f"{name}: {what} must be fp16 or bf16 rows like the others, got {t.dtype} {tuple(t.shape)}")
+        if t.stride(1) != 1:
+            raise HaqError(f"{name}: the channels of {what} must be next to each other, got strides {tuple(t.stride())}")
+        _here(name, what, t)
+    return _DTYPES[first.dtype]
+
+
+def _ld(t):
+    """Row stride; a single row's own length, whatever stride it carries."""
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _here(name, what, t):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise HaqError(f"{name}: {what} is on {t.device}, not on the current GPU")
+
+
+def _flat(name, what, t, dtype, n):
+    """A caller's contiguous buffer of at least n elements."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise HaqError(f"{name}: {what} must be a contiguous {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)}")
+    _here(name, what, t)
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def haq_quant_weight_fp8(w, *, wq=None, w_scale=None):
+    """w fp32 [K,N] -> (wq float8_e4m3fn [K,N] canonical, for haq_pack_weight; w_scale [ceil(K/128), ceil(N/128)])."""
+    K, N = w.shape
+    if w.dtype != torch.float32 or not w.is_contiguous():
+        raise HaqError(f"haq_quant_weight_fp8: w must be a contiguous fp32 matrix, got {w.dtype} with strides {tuple(w.stride())}")
+    _here("haq_quant_weight_fp8", "w", w)
+    if wq is None:
+        wq = torch.empty((K, N), dtype=torch.float8_e4m3fn, device=w.device)
+    if w_scale is None:
+        w_scale = torch.empty((_blocks(K), _blocks(N)), dtype=torch.float32, device=w.device)
+    _flat("haq_quant_weight_fp8", "wq", wq, torch.float8_e4m3fn, K * N)
+    _flat("haq_quant_weight_fp8", "w_scale", w_scale, torch.float32, _blocks(K) * _blocks(N))
+    _check(lib().haq_quant_weight_fp8(_ptr(w), K, N, _ptr(wq), _ptr(w_scale), _stream()))
+    return wq, w_scale
+
+
+def haq_act_scales_fp8_bytes(T: int, K: int) -> int:
+    return int(lib().haq_act_scales_fp8_bytes(T, K))
+
+
+def haq_quant_act_fp8_packed(x, *, q_packed=None, block_scale=None):
+    """x fp16 or bf16 [T,K] -> (codes in the packed operand layout (flat float8_e4m3fn), block_scale (flat fp32, [ceil(K/128)][R]))."""
+    T, K = x.shape
+    dtype = _rows16("haq_quant_act_fp8_packed", x=x)
+    R = -(-T // 16) * 16 + 256
+    n, n_scale = -(-K // 64) * 64 * R, _blocks(K) * R
+    if q_packed is None:
+        q_packed = torch.empty((n,), dtype=torch.float8_e4m3fn, device=x.device)
+    if block_scale is None:
+        block_scale = torch.empty((n_scale,), dtype=torch.float32, device=x.device)
+    _flat("haq_quant_act_fp8_packed", "q_packed", q_packed, torch.float8_e4m3fn, n)
+    _flat("haq_quant_act_fp8_packed", "block_scale", block_scale, torch.float32, n_scale)
+    _check(lib().haq_quant_act_fp8_packed(_adr(x), _ld(x), dtype, T, K, _adr(q_packed), _adr(block_scale), _stream_adr()))
+    return q_packed, block_scale
+
+
+def _fp8_weights(name, w_packed, w_scale, K, N):
+    n = -(-K // 64) * 64 * (-(-N // 256) * 256)
+    if w_packed.dtype not in (torch.int8, torch.uint8, torch.float8_e4m3fn) or not w_packed.is_contiguous() or w_packed.numel() < n:
+        raise HaqError(f"{name}: w_packed must hold {n} bytes from haq_pack_weight, got {w_packed.dtype} {tuple(w_packed.shape)}")
+    _here(name, "w_packed", w_packed)
+    _flat(name, "w_scale", w_scale, torch.float32, _blocks(K) * _blocks(N))
+
+
+def haq_gemm_fp8_packed(q_packed, block_scale, w_packed, w_scale, T: int, K: int, N: int, act: int = HAQ_ACT_NONE, *,
+                        dtype=torch.float16, out=None):
+    """Codes and scales of haq_quant_act_fp8_packed or haq_rmsnorm_quant -> y [T,N] in `dtype` (that of `out`, if given)."""
+    R = -(-T // 16) * 16 + 256
+    _flat("haq_gemm_fp8_packed", "q_packed", q_packed, torch.float8_e4m3fn, -(-K // 64) * 64 * R)
+    _flat("haq_gemm_fp8_packed", "block_scale", block_scale, torch.float32, _blocks(K) * R)
+    _fp8_weights("haq_gemm_fp8_packed", w_packed, w_scale, K, N)
+    y = out if out is not None else torch.empty((T, N), dtype=dtype, device=q_packed.device)
+    number = _rows16("haq_gemm_fp8_packed", out=y)
+    if y.shape != (T, N):
+        raise HaqError(f"haq_gemm_fp8_packed: out is {tuple(y.shape)}, not {(T, N)}")
+    _check(lib().haq_gemm_fp8_packed(_adr(q_packed), _adr(block_scale), _adr(w_packed), _adr(w_scale), T, K, N, act, number,
+                                     _adr(y), _ld(y), _stream_adr()))
+    return y
+
+
+def haq_fp8_linear_workspace_bytes(T: int, K: int, N: int) -> int:
+    return int(lib().haq_fp8_linear_workspace_bytes(T, K, N))
+
+
+def haq_fp8_linear(x, w_packed, w_scale, N: int, act: int = HAQ_ACT_NONE, *, out=None, workspace=None):
+    """x fp16 or bf16 [T,K], weights of haq_quant_weight_fp8 packed with haq_pack_weight -> y [T,N] of x's type."""
+    T, K = x.shape
+    dtype = _rows16("haq_fp8_linear", x=x)
+    _fp8_weights("haq_fp8_linear", w_packed, w_scale, K, N)
+    y = out if out is not None else torch.empty((T, N), dtype=x.dtype, device=x.device)
+    if y.shape != (T, N) or _rows16("haq_fp8_linear", out=y) != dtype:
+        raise HaqError(f"haq_fp8_linear: out is {y.dtype} {tuple(y.shape)}, not {x.dtype} {(T, N)}")
+    if workspace is None:
+        workspace = _ws(haq_fp8_linear_workspace_bytes(T, K, N), x.device)
+    _check(lib().haq_fp8_linear(_adr(x), _ld(x), dtype, _adr(w_packed), _adr(w_scale), T, K, N, act, _adr(y), _ld(y),
+                                _adr(workspace), workspace.numel() * workspace.element_size(), _stream_adr()))
+    return y
+
+
+def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, residual=None, sum_out=None, y=None, q_packed=None,
+                      scale=None):
+    """x fp16 or bf16 [T,K] (+ residual) -> (y, sum, q_packed, scale), None for what was not asked for: y is computed if it is
+    given or no codes are asked for, the sum whenever there is a residual; codes HAQ_CODES_I8 (flat int8, scale [T]) or HAQ_CODES_E4M3
+    (flat float8_e4m3fn, scale flat [ceil(K/128)][R]) in the packed operand layout."""
+    T, K = x.shape
+    dev = x.device
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty((T, K), dtype=x.dtype, device=dev)
+    if y is None and codes == HAQ_CODES_NONE:
+        y = torch.empty((T, K), dtype=x.dtype, device=dev)
+    dtype = _rows16("haq_rmsnorm_quant", x=x, residual=residual, sum_out=sum_out, y=y)
+    _flat("haq_rmsnorm_quant", "weight", weight, torch.float32, K)
+    if codes in (HAQ_CODES_I8, HAQ_CODES_E4M3):
+        R = -(-T // 16) * 16 + 256
+        e4m3 = codes == HAQ_CODES_E4M3
+        n, n_scale, q_type = -(-K // 64) * 64 * R, _blocks(K) * R if e4m3 else T, torch.float8_e4m3fn if e4m3 else torch.int8
+        if q_packed is None:
+            q_packed = torch.empty((n,), dtype=q_type, device=dev)
+        if scale is None:
+            scale = torch.empty((n_scale,), dtype=torch.float32, device=dev)
+        _flat("haq_rmsnorm_quant", "q_packed", q_packed, q_type, n)
+        _flat("haq_rmsnorm_quant", "scale", scale, torch.float32, n_scale)
+    _check(lib().haq_rmsnorm_quant(_adr(x), _ld(x), _adr(residual), _ld(residual), _adr(weight), eps, dtype, T, K, _adr(sum_out),
+                                   _ld(sum_out), _adr(y), _ld(y), codes, _adr(q_packed), _adr(scale), _stream_adr()))
+    return y, sum_out, q_packed, scale
 
 
 def haq_ffn_workspace_bytes(T: int, K: int, F: int, N: int) -> int:

@@ -1,0 +1,214 @@
+// Root-mean-square norm with the residual's addition, and codes as output: the step between two layers that feeds a linear on
+// 8-bit codes (int8 with a scale for each token, or e4m3 with a scale for 128 channels of a token).
+//
+//   h = round16(x + residual);  inv = binary32(1 / sqrt(sum h^2 / K + eps)), in binary64 up to that rounding;
+//   v = (h inv) weight;  y = round16(v);  codes of v (not of y: one rounding fewer).
+//
+// Bound: memory, 2 to 4 reads and writes of 16 bits and one of 8 an element.  A row is read once: it stays in registers as
+// 16-bit values between the sum of squares, the row maximum (int8) and the rounding.  The squares of 16-bit values are exact
+// in binary64 and so are summed there: the rounded root does not depend on the order of the sum (but for one row in some ten
+// million), and the binary64 units of this chip are as wide as the binary32 ones.
+#include "fp8.h"
+
+namespace haq {
+
+namespace {
+
+constexpr int NORM_WAVES = 16;  // most waves of a work-group
+
+template <int CTRL>
+__device__ __forceinline__ double lanes_f64(double v) {
+    const uint64_t u = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+
+// h = round16(x + residual), eight values.  In binary16 the sum of two values rounds the same at once or by way of binary32
+// (24 bits >= 2 * 11 + 2).
+template <int DT>
+__device__ __forceinline__ uint4 add16(const uint4& x, const uint4& r) {
+    if constexpr (DT == HAQ_F16) {
+        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        const h8 s = *reinterpret_cast<const h8*>(&x) + *reinterpret_cast<const h8*>(&r);
+        return *reinterpret_cast<const uint4*>(&s);
+    } else {
+        float a[8], b[8];
+        unpack8<DT>(x, a);
+        unpack8<DT>(r, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = a[i] + b[i];
+        return pack8<DT>(a);
+    }
+}
+
+// A work-group holds RW rows; each of its waves 64 / RW chunks of 16 channels of all of them, a chunk to a lane, NB times.
+// RW = 8: the codes of 8 rows fill the 128-byte lines of the packed layout.
+template <int DT, int RW, int NB>
+__global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
+    constexpr int LPR = 64 / RW;  // lanes of a wave that share a row
+    __shared__ double sums[NORM_WAVES][RW];
+    __shared__ float maxima[NORM_WAVES][RW];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    const int rl = lane / LPR, row = blockIdx.x * RW + rl;
+    const int nchunk = a.K / 16;
+    const bool live = row < a.T;
+    const size_t r = live ? row : 0;
+    auto chunk = [&](int b) { return (b * nw + wave) * LPR + lane % LPR; };
+
+    uint4 h[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int c = chunk(b);
+        h[b][0] = h[b][1] = make_uint4(0, 0, 0, 0);
+        if (live && c < nchunk) {
+            const uint4* px = reinterpret_cast<const uint4*>((const uint16_t*)a.x + r * a.ldx + c * 16);
+            h[b][0] = px[0];
+            h[b][1] = px[1];
+        }
+    }
+    if (a.residual) {
+        uint4 s[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int c = chunk(b);
+            s[b][0] = s[b][1] = make_uint4(0, 0, 0, 0);
+            if (live && c < nchunk) {
+                const uint4* pr = reinterpret_cast<const uint4*>((const uint16_t*)a.residual + r * a.ldr + c * 16);
+                s[b][0] = pr[0];
+                s[b][1] = pr[1];
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            h[b][0] = add16<DT>(h[b][0], s[b][0]);
+            h[b][1] = add16<DT>(h[b][1], s[b][1]);
+        }
+    }
+    double ss = 0.0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float v[16];
+        unpack8<DT>(h[b][0], v);
+        unpack8<DT>(h[b][1], v + 8);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+    }
+    ss += lanes_f64<HAQ_LANES_XOR1>(ss);
+    ss += lanes_f64<HAQ_LANES_XOR2>(ss);
+    ss += lanes_f64<HAQ_LANES_MIRROR8>(ss);
+    if (LPR >= 16) ss += lanes_f64<HAQ_LANES_MIRROR16>(ss);
+    if (LPR >= 32) ss += __shfl_xor(ss, 16);
+    if (LPR >= 64) ss += __shfl_xor(ss, 32);
+    if (lane % LPR == 0) sums[wave][rl] = ss;
+    __syncthreads();
+    // every input has been read: outputs may take the place of x and residual
+    if (a.sum && live) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int c = chunk(b);
+            if (c < nchunk) {
+                uint4* p = reinterpret_cast<uint4*>((uint16_t*)a.sum + r * a.lds + c * 16);
+                p[0] = h[b][0];
+                p[1] = h[b][1];
+            }
+        }
+    }
+    ss = 0.0;
+    for (int w = 0; w < nw; ++w) ss += sums[w][rl];
+    const float inv = (float)(1.0 / sqrt(ss / (double)a.K + a.eps));
+
+    auto norm = [&](int b, float (&v)[16]) {
+        const int c = chunk(b);
+        unpack8<DT>(h[b][0], v);
+        unpack8<DT>(h[b][1], v + 8);
+        const float4* pg = reinterpret_cast<const float4*>(a.weight + (c < nchunk ? c : 0) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 g = pg[i];
+            v[4 * i] = (v[4 * i] * inv) * g.x;
+            v[4 * i + 1] = (v[4 * i + 1] * inv) * g.y;
+            v[4 * i + 2] = (v[4 * i + 2] * inv) * g.z;
+            v[4 * i + 3] = (v[4 * i + 3] * inv) * g.w;
+        }
+    };
+    uint32_t top = 0;  // int8: largest magnitude, as bits, so that infinities and NaN (larger yet) show in it
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int c = chunk(b);
+        const bool here = live && c < nchunk;
+        float v[16];
+        norm(b, v);
+        if (a.y && here) {
+            uint4* p = reinterpret_cast<uint4*>((uint16_t*)a.y + r * a.ldy + c * 16);
+            p[0] = pack8<DT>(v);
+            p[1] = pack8<DT>(v + 8);
+        }
+        if (a.codes == HAQ_CODES_E4M3) {
+            const BlockScale s = block_scale(max_of_8_lanes(here ? absmax16(v) : 0.0f));
+            if (here) {
+                *reinterpret_cast<uint4*>(a.q + ((size_t)c * a.R + row) * 16) = e4m3x16(v, s.r);
+                if (c % 8 == 0) a.scale[(size_t)(c / 8) * a.R + row] = s.scale;
+            }
+        } else if (a.codes == HAQ_CODES_I8 && here) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
+    }
+    if (a.codes != HAQ_CODES_I8) return;
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if (lane % LPR == 0) maxima[wave][rl] = __uint_as_float(top);
+    __syncthreads();
+    for (int w = 0; w < nw; ++w) top = max(top, __float_as_uint(maxima[w][rl]));
+    const float amax = __uint_as_float(top);
+    const bool zero = !(amax >= TINY_MAX && amax < __builtin_inff());
+    const float scale = amax < TINY_MAX ? 0.0f : amax / 127.0f, rscale = 1.0f / scale;
+    const bool fast = scale >= 0x1p-100f && scale <= 0x1p100f;
+    if (live && wave == 0 && lane % LPR == 0) a.scale[row] = scale;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int c = chunk(b);
+        float v[16];
+        norm(b, v);
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (!zero) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = fast ? div_by(v[i], scale, rscale, true) : fminf(fmaxf(v[i] / scale, -127.0f), 127.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = round_pack4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+        if (live && c < nchunk) *reinterpret_cast<uint4*>(a.q + ((size_t)c * a.R + row) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <int DT, int RW, int NB>
+int launch_one(const NormArgs& a, int waves, hipStream_t st) {
+    hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB>), dim3((unsigned)cdiv(a.T, RW)), dim3(waves * 64), 0, st, a);
+    HAQ_CHECK_HIP(hipGetLastError());
+    return HAQ_OK;
+}
+
+template <int DT, int RW>
+int launch_rows(const NormArgs& a, hipStream_t st) {
+    const int per_wave = 64 / RW, need = cdiv(a.K / 16, per_wave);  // wave-wide pieces of a row
+    if (need <= NORM_WAVES) return launch_one<DT, RW, 1>(a, need, st);
+    if (need <= 2 * NORM_WAVES) return launch_one<DT, RW, 2>(a, cdiv(need, 2), st);
+    if (need <= 4 * NORM_WAVES) return launch_one<DT, RW, 4>(a, cdiv(need, 4), st);
+    if constexpr (RW == 8) return launch_one<DT, RW, 8>(a, cdiv(need, 8), st);
+    return HAQ_ERR_UNSUPPORTED;
+}
+
+template <int DT>
+int launch_type(const NormArgs& a, hipStream_t st) {
+    if (a.K <= 16384 && a.T >= 8 * cu_count()) return launch_rows<DT, 8>(a, st);
+    return launch_rows<DT, 1>(a, st);
+}
+
+}  // namespace
+
+int launch_rmsnorm(const NormArgs& a, int dtype, hipStream_t st) {
+    return dtype == HAQ_F16 ? launch_type<HAQ_F16>(a, st) : launch_type<HAQ_BF16>(a, st);
+}
+
+}  // namespace haq
