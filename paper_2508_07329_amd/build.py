@@ -9,7 +9,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhaq.so")
 SOURCES = ["api.hip", "quant.hip", "gemm.hip", "skinny.hip", "moe.hip", "decode.hip", "search.hip", "sched.hip", "hessian.hip", "probe.hip", "cpu_expert.hip",
-           "fp8_api.hip", "fp8_quant.hip", "fp8_gemm.hip", "rmsnorm.hip"]
+           "fp8_api.hip", "fp8_quant.hip", "fp8_gemm.hip", "fp8_stream.hip", "rmsnorm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -50,6 +50,10 @@ struct Fp8GemmArgs {
     int64_t ldy;
 };
 int launch_fp8_gemm(const Fp8GemmArgs& a, int dtype, hipStream_t st);
+bool fp8_stream_rows16_fits(int M, int K);  // a few rows in 16 bits: codes and linear in one launch (A, sa and R of `a` not used)
+int launch_fp8_stream_rows16(const Fp8GemmArgs& a, const void* x, int64_t ldx, int dtype, hipStream_t st);
+// The streaming kernel in tiles of 16 row_blocks rows x 16 channel_blocks channels: 1 x 1, 1 x 2, 1 x 4, 2 x 2, 2 x 4, 4 x 2 or 4 x 4.
+int launch_fp8_stream(const Fp8GemmArgs& a, int row_blocks, int channel_blocks, int dtype, hipStream_t st);
 
 // ---- device ----------------------------------------------------------------------------------------------------
 #ifdef __HIPCC__

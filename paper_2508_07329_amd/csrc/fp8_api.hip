@@ -105,8 +105,10 @@ int32_t haq_fp8_linear(const void* x, int64_t ldx, int32_t dtype, const uint8_t*
         HAQ_FAIL(HAQ_ERR_WORKSPACE, "haq_fp8_linear: workspace of %zu bytes (256-byte aligned) needed, got %zu", need, workspace_bytes);
     uint8_t* q = (uint8_t*)workspace;
     float* sa = (float*)(q + scales_at(T, K));
+    const Fp8GemmArgs a = gemm_args(q, sa, w_packed, w_scale, T, K, N, act, y, ldy);
+    if (fp8_stream_rows16_fits(T, K)) return launch_fp8_stream_rows16(a, x, ldx, dtype, (hipStream_t)stream);
     if (const int rc = launch_act_quant_fp8({x, ldx, T, K, q, act_rows(T), sa}, dtype, (hipStream_t)stream)) return rc;
-    return launch_fp8_gemm(gemm_args(q, sa, w_packed, w_scale, T, K, N, act, y, ldy), dtype, (hipStream_t)stream);
+    return launch_fp8_gemm(a, dtype, (hipStream_t)stream);
 }
 
 int32_t haq_rmsnorm_quant(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, double eps, int32_t dtype,

@@ -1,0 +1,291 @@
+// Tiled kernel of the 8-bit floating-point linear (many token rows):
+//   y[t][n] = round16(act(sum_b (sa[b][t] sb[b][n / 128]) p_b[t][n])),  p_b = the products of the 128 channels of block b.
+//
+// Data flow of a work-group (BM x BN output tile, WAVES_M x WAVES_N waves of 64 x WN): a block of 128 channels is a K-step.
+//   HBM/L2 --buffer_load ... lds--> a ring of LDS stages (codes of BM tokens and BN channels, chunk-major as in memory, and the
+//   tokens' scales) --ds_read_b128--> fragments --> v_mfma_f32_16x16x128_f8f6f4, which forms p_b for 16 tokens x 16 channels at
+//   once --> one fused multiply-add by the block's scale into the binary32 sum.
+// The weights are the first operand, so a lane owns one token (one scale) and four consecutive channels; a wave's channels lie in
+// one block of 128, so their scale is a scalar.
+#pragma once
+#include "fp8.h"
+
+namespace haq {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ v4f mfma_e4m3(v8i w, v8i x, v4f c) { return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0); }
+
+// s_waitcnt immediates: vmcnt in bits [3:0] and [15:14], lgkmcnt in [11:8]; LDS reads complete, at most n loads on their way
+#define HAQ_FP8_WAIT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | (((n) >> 4) << 14) | (0x7 << 4))
+#define HAQ_FP8_FENCE() asm volatile("" ::: "memory")
+
+// Buffer resources (device side only): a lane's address is a scalar base, its own 32-bit offset and a scalar one; a lane
+// whose offset lies past the resource's bytes fetches zeros.
+#ifdef __HIP_DEVICE_COMPILE__
+typedef __amdgpu_buffer_rsrc_t Fp8Rsrc;
+__device__ __forceinline__ Fp8Rsrc fp8_rsrc(const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000); }
+__device__ __forceinline__ void fp8_to_lds16(Fp8Rsrc r, int8_t* to, uint32_t lane_off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, lane_off, 0, 0, 0);
+}
+__device__ __forceinline__ void fp8_to_lds4(Fp8Rsrc r, int8_t* to, uint32_t lane_off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 4, lane_off, 0, 0, 0);
+}
+#else
+typedef const void* Fp8Rsrc;
+__device__ __forceinline__ Fp8Rsrc fp8_rsrc(const void* p, uint32_t) { return p; }
+__device__ __forceinline__ void fp8_to_lds16(Fp8Rsrc, int8_t*, uint32_t) {}
+__device__ __forceinline__ void fp8_to_lds4(Fp8Rsrc, int8_t*, uint32_t) {}
+#endif
+constexpr uint32_t FP8_PAST_END = 0xFFFF0000u;  // an offset past every resource's bytes
+
+// Work-group id -> tile: ids go round-robin to the 8 XCDs; each of them (one L2) takes a contiguous range of tiles, in bands
+// of row tiles (1024 rows), rows fastest inside a band, so that what an XCD holds at a time shares rows and channels.
+template <int BM, int BN>
+__device__ __forceinline__ bool fp8_tile(const Fp8GemmArgs& a, int& m0, int& n0) {
+    constexpr int BAND = 1024 / BM;
+    const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN, total = mt * nt, per = (total + 7) / 8;
+    const int slot = blockIdx.x / 8, id = (int)(blockIdx.x % 8) * per + slot;
+    if (slot >= per || id >= total) return false;
+    const int band = id / (BAND * nt), rem = id % (BAND * nt), rows = min(BAND, mt - band * BAND);
+    m0 = (band * BAND + rem % rows) * BM;
+    n0 = rem / rows * BN;
+    return true;
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG>
+struct Fp8Shape {
+    static constexpr int NW = WAVES_M * WAVES_N, THREADS = KG * NW * 64;
+    static constexpr int STAGE_BYTES = (BM + BN) * FP8_BLOCK + NW * 256;  // codes; 64 token scales for each wave
+    static constexpr int LDS_BYTES = KG * STAGES * STAGE_BYTES;
+};
+
+// KG: groups of waves that share the tile and take its K-steps in turn, each with a ring of its own; their sums are added at the end.
+template <int DT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG, int MINB>
+__global__ __launch_bounds__(KG * WAVES_M * WAVES_N * 64, MINB) void fp8_gemm_kernel(Fp8GemmArgs a) {
+    using S = Fp8Shape<BM, BN, WAVES_M, WAVES_N, STAGES, KG>;
+    constexpr int NW = S::NW, STAGE = S::STAGE_BYTES;
+    constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, MI = WM / 16, NJ = WN / 16, NP = NJ / 2;
+    constexpr int GA = 8 * BM / 64, GB = 8 * BN / 64, LPA = GA / NW, LPB = GB / NW, LOADS = LPA + LPB + 1;
+    static_assert((WM == 64 || WM == 32) && (WN == 64 || WN == 128) && GA % NW == 0 && GB % NW == 0, "at most 64 scales and one block of channels to a wave");
+    static_assert(NPAD % BN == 0 && BM <= 256, "the packed operands are padded for the tile");
+    constexpr int M = 2 * MI * NP, RING = 4, LAG = RING - 1;  // matrix instructions of a K-step; products in flight
+    static_assert(M % RING == 0, "the ring is back at its start after a K-step");
+    constexpr int SPAN = NP == 2 ? 2 * MI : 4 * MI;  // matrix instructions that the loads of a K-step are spread over, from the barrier on
+    constexpr int PITCH = WN * 2 + 8;
+    static_assert(STAGES >= 2 && (STAGES - 2) * LOADS <= 63, "s_waitcnt counts the loads of a whole ring");
+    constexpr int EXCHANGE = KG == 2 ? BM * BN * 4 : 0;
+    static_assert(KG == 1 || (KG == 2 && MI % 2 == 0), "two groups store half of the rows each");
+    static_assert(EXCHANGE + KG * NW * 16 * PITCH <= S::LDS_BYTES, "epilogue staging");
+    extern __shared__ __attribute__((aligned(1024))) int8_t all_lds[];
+
+    int m0, n0;
+    if (!fp8_tile<BM, BN>(a, m0, n0)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = KG == 1 ? 0 : wave_id / NW, wave = KG == 1 ? wave_id : wave_id % NW;
+    int8_t* lds = all_lds + kg * STAGES * STAGE;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N, l16 = lane & 15, q = lane >> 4;
+    const int nkt = (a.K + FP8_BLOCK - 1) / FP8_BLOCK, nn = (a.N + FP8_BLOCK - 1) / FP8_BLOCK;
+
+    // Loads of a K-step: LPA groups of 64 tokens x 16 bytes, LPB of 64 channels x 16 bytes, and the wave's 64 token scales.
+    // Lane offsets are from the K-step's first chunk, whose address the resources carry in 64 bits; their sizes end with K, so that
+    // chunks past it are zeros.
+    uint32_t off[LPA + LPB];
+#pragma unroll
+    for (int i = 0; i < LPA; ++i) {
+        const int g = wave + i * NW, row = m0 + g % (BM / 64) * 64 + lane;
+        off[i] = row < a.M ? (uint32_t)((size_t)(g / (BM / 64)) * a.R + row) * 16 : FP8_PAST_END;
+    }
+#pragma unroll
+    for (int i = 0; i < LPB; ++i) {
+        const int g = wave + i * NW;
+        off[LPA + i] = (uint32_t)((size_t)(g / (BN / 64)) * a.Npad + n0 + g % (BN / 64) * 64 + lane) * 16;
+    }
+    const uint32_t chunk_a = (uint32_t)a.R * 16, chunk_b = (uint32_t)a.Npad * 16;  // bytes
+    const uint8_t* pa = a.A + (size_t)kg * 8 * chunk_a;
+    const uint8_t* pb = a.B + (size_t)kg * 8 * chunk_b;
+    const float* ps = a.sa + m0 + wm * WM + kg * a.R;  // (64 scales whatever WM is: the rows' padding covers them)
+    // chunks of 16 channels from the K-step to be requested on (the weights are padded to whole 64 channels, but what meets no token
+    // chunk counts for nothing)
+    int left = max(0, a.K / 16 - 8 * kg);
+    uint32_t bytes_a, bytes_b, bytes_s;
+    auto sizes = [&]() __attribute__((always_inline)) {
+        asm("" : "+s"(left));  // a clamp on both sides would become a vector instruction, and the sizes divergent
+        const uint32_t c = (uint32_t)min(8, left);
+        bytes_a = c * chunk_a;
+        bytes_b = c * chunk_b;
+        bytes_s = left > 0 ? 256 : 0;
+    };
+    sizes();
+    auto load = [&](int stage_at, int i) __attribute__((always_inline)) {
+        int8_t* stage = lds + stage_at;
+        if (i < LPA)
+            fp8_to_lds16(fp8_rsrc(pa, bytes_a), stage + (wave + i * NW) * 1024, off[i]);
+        else if (i < LPA + LPB)
+            fp8_to_lds16(fp8_rsrc(pb, bytes_b), stage + BM * FP8_BLOCK + (wave + (i - LPA) * NW) * 1024, off[i]);
+        else
+            fp8_to_lds4(fp8_rsrc(ps, bytes_s), stage + (BM + BN) * FP8_BLOCK + wave * 256, lane * 4);
+    };
+    auto advance = [&]() __attribute__((always_inline)) {
+        pa += (size_t)KG * 8 * chunk_a;
+        pb += (size_t)KG * 8 * chunk_b;
+        ps += KG * a.R;
+        left = max(0, left - KG * 8);
+        sizes();
+    };
+
+    v4f acc[MI][NJ], p[RING];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < RING; ++i) p[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v8i fa[MI], fb[2][2];
+    float sx[MI], s[MI], old[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) s[i] = 0.0f;
+    const int frag_a = (2 * q * BM + wm * WM + l16) * 16, frag_b = BM * FP8_BLOCK + (2 * q * BN + wn * WN + l16) * 16;
+    const int scale_at = (BM + BN) * FP8_BLOCK + wave * 256 + l16 * 4;
+    auto read = [&](v8i& f, int at, int rows) __attribute__((always_inline)) {  // two chunks of 16 channels
+        typedef int v4i __attribute__((ext_vector_type(4)));
+        const v4i lo = *reinterpret_cast<const v4i*>(lds + at), hi = *reinterpret_cast<const v4i*>(lds + at + rows * 16);
+        f = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    typedef const __attribute__((address_space(4))) float* ScalarPtr;
+    ScalarPtr psw = (ScalarPtr)(uintptr_t)(a.sb + (size_t)min(kg, nkt - 1) * nn + min((n0 + wn * WN) / FP8_BLOCK, nn - 1));
+    float sw = psw[0];
+    int more = nkt - 1 - kg;  // K-steps behind the present one
+
+    // The sum takes product m LAG instructions after it was issued, when it is there; the last ones of a K-step, with its scales, in
+    // the next.  Order: pairs of channel blocks, tokens, the two of a pair; so a token fragment is last used well before the next K-step.
+    auto add = [&](int m, const float (&sc)[MI]) __attribute__((always_inline)) {
+        const int j = m / (2 * MI) * 2 + m % 2, i = m / 2 % MI;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(sc[i], p[m % RING][r], acc[i][j][r]);
+    };
+    auto step = [&](int prv, int cur, int nxt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            old[i] = s[i];
+            s[i] = sx[i] * sw;
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int jp = m / (2 * MI), mm = m % (2 * MI), i = mm / 2;
+            if (mm == 0 && jp == NP - 1) {
+                // this wave's reads of the stage are complete and its part of the next one has landed; behind the barrier that holds
+                // for every wave: the stage may be overwritten, the next one read
+                HAQ_FP8_WAIT((STAGES - 2) * LOADS);
+                HAQ_FP8_FENCE();
+                __builtin_amdgcn_s_barrier();
+                HAQ_FP8_FENCE();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            p[m % RING] = mfma_e4m3(fb[jp & 1][m % 2], fa[i], v4f{0.0f, 0.0f, 0.0f, 0.0f});
+            __builtin_amdgcn_sched_barrier(0);
+            if (m < LAG)
+                add(M - LAG + m, old);
+            else
+                add(m - LAG, s);
+            if (mm < 2) {  // the next pair of channel blocks
+                const int at = jp == NP - 1 ? nxt + frag_b : cur + frag_b + (jp + 1) * 2 * 256;
+                read(fb[(jp + 1) & 1][mm], at + mm * 256, BN);
+            }
+            if (jp == NP - 1) {
+                if (mm % 2 == 1) read(fa[i], nxt + frag_a + i * 256, BM);
+                if (mm >= 2 && mm < 2 + MI) sx[mm - 2] = *reinterpret_cast<const float*>(lds + nxt + scale_at + (mm - 2) * 64);
+            }
+            // loads of K-step kt + STAGES, from behind the barrier on, into the stage that this K-step leaves (jp = NP - 1); the rest of
+            // them with the next K-step
+            const int at = (m + 2 * MI) % M;
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l)
+                if (l * SPAN / LOADS == at && at < SPAN) load(jp == NP - 1 ? cur : prv, l);
+            if (m == 2 * MI - 1) advance();
+            if (m == (NP - 2) * 2 * MI + 2) {  // behind this pair's LDS reads: a scalar load among them would make their waits wait for all
+                psw += more >= KG ? KG * nn : 0;
+                more -= KG;
+                sw = psw[0];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // K-steps 0 .. STAGES - 2 and the first part of the loads of the next, as the loop leaves them
+#pragma unroll
+    for (int t = 0; t < STAGES - 1; ++t) {
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) load(t * STAGE, l);
+        advance();
+    }
+    HAQ_FP8_WAIT((STAGES - 2) * LOADS);
+    HAQ_FP8_FENCE();
+    __builtin_amdgcn_s_barrier();
+    HAQ_FP8_FENCE();
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l)
+        if (l * SPAN / LOADS < 2 * MI) load((STAGES - 1) * STAGE, l);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        read(fa[i], frag_a + i * 256, BM);
+        sx[i] = *reinterpret_cast<const float*>(lds + scale_at + i * 64);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) read(fb[0][j], frag_b + j * 256, BN);
+
+    int prv = (STAGES - 1) * STAGE, cur = 0;
+    for (int kt = 0; kt < nkt; kt += KG) {  // the same number of K-steps for every group: past the last one operands and scales are zeros
+        const int nxt = cur == (STAGES - 1) * STAGE ? 0 : cur + STAGE;
+        step(prv, cur, nxt);
+        prv = cur;
+        cur = nxt;
+    }
+#pragma unroll
+    for (int m = M - LAG; m < M; ++m) add(m, s);
+
+    // ---- epilogue: lane l holds token row i*16 + l%16, channels j*16 + 4*(l/16) .. + 3 of the wave tile
+    HAQ_FP8_WAIT(0);  // the loads past the last K-step
+    HAQ_FP8_FENCE();
+    __builtin_amdgcn_s_barrier();
+    HAQ_FP8_FENCE();
+    if constexpr (KG == 2) {  // each group adds up and stores half of the token rows
+        v4f* half = reinterpret_cast<v4f*>(all_lds);
+        auto at = [&](int from, int i, int j) { return (((from * NW + wave) * (MI / 2) + i) * NJ + j) * 64 + lane; };
+#pragma unroll
+        for (int i = 0; i < MI / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) half[at(kg, i, j)] = kg ? acc[i][j] : acc[MI / 2 + i][j];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MI / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = (kg ? acc[MI / 2 + i][j] : acc[i][j]) + half[at(1 - kg, i, j)];
+    }
+    int8_t* stage = all_lds + EXCHANGE + wave_id * 16 * PITCH;  // private to the wave, 16 rows at a time
+    const int first_row = m0 + wm * WM + kg * (WM / 2);
+    constexpr int LANES_PER_ROW = WN * 2 / 16, ROWS_PER_IT = 64 / LANES_PER_ROW;
+#pragma unroll
+    for (int i = 0; i < MI / KG; ++i) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            float v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = a.act == HAQ_ACT_RELU && acc[i][j][r] < 0.0f ? 0.0f : acc[i][j][r];
+            *reinterpret_cast<uint2*>(stage + l16 * PITCH + (j * 16 + 4 * q) * 2) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+        }
+        HAQ_FP8_FENCE();  // LDS serves one wave's requests in order
+#pragma unroll
+        for (int it = 0; it < 16 / ROWS_PER_IT; ++it) {
+            const int r2 = it * ROWS_PER_IT + lane / LANES_PER_ROW, c8 = lane % LANES_PER_ROW * 8;
+            const int row = first_row + i * 16 + r2, col = n0 + wn * WN + c8;
+            const uint2 v0 = *reinterpret_cast<const uint2*>(stage + r2 * PITCH + c8 * 2);
+            const uint2 v1 = *reinterpret_cast<const uint2*>(stage + r2 * PITCH + c8 * 2 + 8);
+            if (row < a.M && col < a.N) *reinterpret_cast<uint4*>((uint16_t*)a.Y + (size_t)row * a.ldy + col) = make_uint4(v0.x, v0.y, v1.x, v1.y);
+        }
+        HAQ_FP8_FENCE();
+    }
+}
+
+}  // namespace haq

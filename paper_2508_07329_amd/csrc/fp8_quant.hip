@@ -11,11 +11,10 @@ constexpr int AQ_WAVES = 4;
 // of a block, whose maximum takes three lane exchanges, and with RW = 8 the codes of 8 rows fill the 128-byte lines of the
 // packed layout.  Bound: memory, two bytes read and one written an element.
 template <int DT, int RW>
-__global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a, int pieces) {
+__global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a) {
     constexpr int LPR = 64 / RW;
     const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * AQ_WAVES + (threadIdx.x >> 6);
-    const int row = (int)(id / pieces) * RW + lane / LPR, c = (int)(id % pieces) * LPR + lane % LPR;
+    const int row = (int)blockIdx.x * RW + lane / LPR, c = ((int)blockIdx.y * AQ_WAVES + (threadIdx.x >> 6)) * LPR + lane % LPR;
     const bool here = row < a.T && c < a.K / 16;
     float v[16] = {};
     if (here) {
@@ -34,8 +33,7 @@ __global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a
 template <int DT, int RW>
 int launch_act(const ActQuantArgs& a, hipStream_t st) {
     const int pieces = cdiv(a.K / 16, 64 / RW);
-    hipLaunchKernelGGL((act_quant_kernel<DT, RW>), dim3((unsigned)cdiv((int64_t)cdiv(a.T, RW) * pieces, AQ_WAVES)), dim3(AQ_WAVES * 64), 0, st, a,
-                       pieces);
+    hipLaunchKernelGGL((act_quant_kernel<DT, RW>), dim3(cdiv(a.T, RW), cdiv(pieces, AQ_WAVES)), dim3(AQ_WAVES * 64), 0, st, a);
     HAQ_CHECK_HIP(hipGetLastError());
     return HAQ_OK;
 }

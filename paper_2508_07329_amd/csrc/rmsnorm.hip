@@ -14,7 +14,8 @@ namespace haq {
 
 namespace {
 
-constexpr int NORM_WAVES = 16;  // most waves of a work-group
+constexpr int NORM_WAVES = 16;             // most waves of a work-group
+constexpr int MAX_GROUPS_X = 1 << 20;      // a grid has fewer than 2^32 threads in a direction
 
 template <int CTRL>
 __device__ __forceinline__ double lanes_f64(double v) {
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
     __shared__ double sums[NORM_WAVES][RW];
     __shared__ float maxima[NORM_WAVES][RW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    const int rl = lane / LPR, row = blockIdx.x * RW + rl;
+    const int rl = lane / LPR, row = (int)(blockIdx.y * gridDim.x + blockIdx.x) * RW + rl;
     const int nchunk = a.K / 16;
     const bool live = row < a.T;
     const size_t r = live ? row : 0;
@@ -184,7 +185,8 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
 
 template <int DT, int RW, int NB>
 int launch_one(const NormArgs& a, int waves, hipStream_t st) {
-    hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB>), dim3((unsigned)cdiv(a.T, RW)), dim3(waves * 64), 0, st, a);
+    const int groups = cdiv(a.T, RW), x = groups < MAX_GROUPS_X ? groups : MAX_GROUPS_X;
+    hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB>), dim3(x, cdiv(groups, x)), dim3(waves * 64), 0, st, a);
     HAQ_CHECK_HIP(hipGetLastError());
     return HAQ_OK;
 }

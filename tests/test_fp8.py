@@ -4,6 +4,7 @@ import torch
 
 import paper_2508_07329_amd as haq
 from tests import fp8_reference as ref
+from tests.fp8_sizes import STREAM, TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -114,6 +115,21 @@ def test_linear(T, K, N, dtype):
     ref.assert_linear(wide[:, :N].cpu(), want, bound)
     assert bool((wide[:, N:] == 7.0).all())
     assert same_bits(y, haq.haq_fp8_linear(x.to(DEV), wp, swd, N, act))  # a call repeated is the same
+
+
+@pytest.mark.parametrize("T,K,N", [size for shapes in (STREAM, TILED) for sizes in shapes.values() for size in sizes])
+def test_linear_on_each_kernel(T, K, N):
+    x = ref.rows(T * K + N, T, K, F16)
+    wq, sw, wp, swd = weights(T + K + N, K, N)
+    q, s = haq.haq_quant_act_fp8_packed(x.to(DEV))
+    want, bound = ref.linear(*ref.act_codes(x.float()), wq, sw)
+    wide = torch.full((T + 1, N + 8), 7.0, dtype=BF16, device=DEV)
+    haq.haq_gemm_fp8_packed(q, s, wp, swd, T, K, N, out=wide[:T, :N])
+    ref.assert_linear(wide[:T, :N].cpu(), want, bound)
+    assert bool((wide[:T, N:] == 7.0).all()) and bool((wide[T] == 7.0).all())
+    again = torch.empty((T, N), dtype=BF16, device=DEV)
+    haq.haq_gemm_fp8_packed(q, s, wp, swd, T, K, N, out=again)
+    assert same_bits(again, wide[:T, :N])
 
 
 @pytest.mark.parametrize("T,K,N", [(1, 400, 272), (20, 1040, 272), (100, 400, 144), (300, 656, 528)])
