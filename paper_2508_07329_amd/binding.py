@@ -145,12 +145,10 @@ def _adr(t):
     return None if t is None else t.data_ptr()
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _stream_adr():
-    if _raw_stream is None:
-        return torch.cuda.current_stream().cuda_stream
     return _raw_stream(torch.cuda.current_device())
 
 
@@ -292,12 +290,15 @@ def haq_gemm_w8a8_packed(q_packed, row_scale, w_packed, w_scale, T: int, K: int,
 
 
 # ---- 8-bit floating point with block scales, and the norm in front of a linear ------------
+# A serving loop makes these calls, and looking a tensor over takes as long as handing it on: each is looked at once, by
+# _ld_like or _fits, and only what does not pass goes to _rows16 or _flat, which say what is wrong with it.
 _DTYPES = {torch.float16: HAQ_F16, torch.bfloat16: HAQ_BF16}
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _rows16(name, **tensors):
-    """The dtype number of 16-bit rows [T, K]; raises if they differ in shape or type, or live on another GPU than the current
-    one (whose stream the work goes to)."""
+    """Raises if 16-bit rows [T, K] differ in shape or type, or live on another GPU than the current one (whose stream the work
+    goes to)."""
     first = None
     for what, t in tensors.items():
         if t is None:
@@ -308,12 +309,6 @@ def _rows16(name, **tensors):
         if t.stride(1) != 1:
             raise HaqError(f"{name}: the channels of {what} must be next to each other, got strides {tuple(t.stride())}")
         _here(name, what, t)
-    return _DTYPES[first.dtype]
-
-
-def _ld(t):
-    """Row stride; a single row's own length, whatever stride it carries."""
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _here(name, what, t):
@@ -322,10 +317,31 @@ def _here(name, what, t):
 
 
 def _flat(name, what, t, dtype, n):
-    """A caller's contiguous buffer of at least n elements."""
+    """Raises unless t is a contiguous buffer of at least n elements."""
     if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
         raise HaqError(f"{name}: {what} must be a contiguous {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)}")
     _here(name, what, t)
+
+
+def _ld_like(t, dtype, shape, dev):
+    """Row stride (a single row's own length, whatever stride it carries) of rows of this type, shape and GPU; -1: they are not."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        return -1
+    ld, one = t.stride()
+    return -1 if one != 1 else ld if shape[0] > 1 else shape[1]
+
+
+def _fits(t, dtype, n, dev):
+    return t.dtype is dtype and t.numel() >= n and t.get_device() == dev and t.is_contiguous()
+
+
+def _first_rows(name, x):
+    """(shape, type, its number, GPU, row stride) of the rows that a call goes by."""
+    shape, s, dtype, dev = x.shape, x.stride(), x.dtype, x.get_device()
+    number = _DTYPES.get(dtype)
+    if number is None or len(s) != 2 or s[1] != 1 or dev < 0 or dev != _current_device():
+        _rows16(name, x=x)
+    return shape, dtype, number, dev, s[0] if shape[0] > 1 else shape[1]
 
 
 def _blocks(n: int) -> int:
@@ -352,43 +368,70 @@ def haq_act_scales_fp8_bytes(T: int, K: int) -> int:
     return int(lib().haq_act_scales_fp8_bytes(T, K))
 
 
+def _codes_buffers(name, T, K, q, scale, q_type, n_scale, dev, x):
+    """The packed codes' buffer and their scales', made or looked over."""
+    n = -(-K // 64) * 64 * (-(-T // 16) * 16 + 256)
+    if q is None:
+        q = torch.empty((n,), dtype=q_type, device=x.device)
+    elif not _fits(q, q_type, n, dev):
+        _flat(name, "q_packed", q, q_type, n)
+    if scale is None:
+        scale = torch.empty((n_scale,), dtype=torch.float32, device=x.device)
+    elif not _fits(scale, torch.float32, n_scale, dev):
+        _flat(name, "scale", scale, torch.float32, n_scale)
+    return q, scale
+
+
 def haq_quant_act_fp8_packed(x, *, q_packed=None, block_scale=None):
     """x fp16 or bf16 [T,K] -> (codes in the packed operand layout (flat float8_e4m3fn), block_scale (flat fp32, [ceil(K/128)][R]))."""
-    T, K = x.shape
-    dtype = _rows16("haq_quant_act_fp8_packed", x=x)
-    R = -(-T // 16) * 16 + 256
-    n, n_scale = -(-K // 64) * 64 * R, _blocks(K) * R
-    if q_packed is None:
-        q_packed = torch.empty((n,), dtype=torch.float8_e4m3fn, device=x.device)
-    if block_scale is None:
-        block_scale = torch.empty((n_scale,), dtype=torch.float32, device=x.device)
-    _flat("haq_quant_act_fp8_packed", "q_packed", q_packed, torch.float8_e4m3fn, n)
-    _flat("haq_quant_act_fp8_packed", "block_scale", block_scale, torch.float32, n_scale)
-    _check(lib().haq_quant_act_fp8_packed(_adr(x), _ld(x), dtype, T, K, _adr(q_packed), _adr(block_scale), _stream_adr()))
-    return q_packed, block_scale
+    (T, K), _, number, dev, ld = _first_rows("haq_quant_act_fp8_packed", x)
+    q, scale = _codes_buffers("haq_quant_act_fp8_packed", T, K, q_packed, block_scale, torch.float8_e4m3fn,
+                              -(-K // 128) * (-(-T // 16) * 16 + 256), dev, x)
+    _check(lib().haq_quant_act_fp8_packed(x.data_ptr(), ld, number, T, K, q.data_ptr(), scale.data_ptr(), _raw_stream(dev)))
+    return q, scale
+
+
+_BYTES = (torch.int8, torch.uint8, torch.float8_e4m3fn)
 
 
 def _fp8_weights(name, w_packed, w_scale, K, N):
     n = -(-K // 64) * 64 * (-(-N // 256) * 256)
-    if w_packed.dtype not in (torch.int8, torch.uint8, torch.float8_e4m3fn) or not w_packed.is_contiguous() or w_packed.numel() < n:
+    if w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.numel() < n:
         raise HaqError(f"{name}: w_packed must hold {n} bytes from haq_pack_weight, got {w_packed.dtype} {tuple(w_packed.shape)}")
     _here(name, "w_packed", w_packed)
     _flat(name, "w_scale", w_scale, torch.float32, _blocks(K) * _blocks(N))
 
 
+def _out_rows(name, out, T, N, dtype, dev, device):
+    """(y, row stride): made, or the caller's."""
+    if out is None:
+        return torch.empty((T, N), dtype=dtype, device=device), N
+    ld = _ld_like(out, dtype, (T, N), dev)
+    if ld < 0:
+        _rows16(name, out=out)
+        raise HaqError(f"{name}: out is {out.dtype} {tuple(out.shape)}, not {dtype} {(T, N)}")
+    return out, ld
+
+
 def haq_gemm_fp8_packed(q_packed, block_scale, w_packed, w_scale, T: int, K: int, N: int, act: int = HAQ_ACT_NONE, *,
-                        dtype=torch.float16, out=None):
-    """Codes and scales of haq_quant_act_fp8_packed or haq_rmsnorm_quant -> y [T,N] in `dtype` (that of `out`, if given)."""
-    R = -(-T // 16) * 16 + 256
-    _flat("haq_gemm_fp8_packed", "q_packed", q_packed, torch.float8_e4m3fn, -(-K // 64) * 64 * R)
-    _flat("haq_gemm_fp8_packed", "block_scale", block_scale, torch.float32, _blocks(K) * R)
-    _fp8_weights("haq_gemm_fp8_packed", w_packed, w_scale, K, N)
-    y = out if out is not None else torch.empty((T, N), dtype=dtype, device=q_packed.device)
-    number = _rows16("haq_gemm_fp8_packed", out=y)
-    if y.shape != (T, N):
-        raise HaqError(f"haq_gemm_fp8_packed: out is {tuple(y.shape)}, not {(T, N)}")
-    _check(lib().haq_gemm_fp8_packed(_adr(q_packed), _adr(block_scale), _adr(w_packed), _adr(w_scale), T, K, N, act, number,
-                                     _adr(y), _ld(y), _stream_adr()))
+                        dtype=None, out=None):
+    """Codes and scales of haq_quant_act_fp8_packed or haq_rmsnorm_quant -> y [T,N] in `dtype` (fp16, or that of `out`)."""
+    name = "haq_gemm_fp8_packed"
+    dev, R = q_packed.get_device(), -(-T // 16) * 16 + 256
+    n, n_scale = -(-K // 64) * 64 * R, -(-K // 128) * R
+    if dev < 0 or dev != _current_device() or not _fits(q_packed, torch.float8_e4m3fn, n, dev) or not _fits(block_scale, torch.float32, n_scale, dev):
+        _flat(name, "q_packed", q_packed, torch.float8_e4m3fn, n)
+        _flat(name, "block_scale", block_scale, torch.float32, n_scale)
+    n = -(-K // 64) * 64 * (-(-N // 256) * 256)
+    if (w_packed.numel() < n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
+            or not _fits(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
+        _fp8_weights(name, w_packed, w_scale, K, N)
+    dtype = dtype or (torch.float16 if out is None else out.dtype)
+    if dtype not in _DTYPES:
+        raise HaqError(f"{name}: dtype must be fp16 or bf16, got {dtype}")
+    y, ld = _out_rows(name, out, T, N, dtype, dev, q_packed.device)
+    _check(lib().haq_gemm_fp8_packed(q_packed.data_ptr(), block_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(), T, K, N, act,
+                                     _DTYPES[dtype], y.data_ptr(), ld, _raw_stream(dev)))
     return y
 
 
@@ -398,16 +441,19 @@ def haq_fp8_linear_workspace_bytes(T: int, K: int, N: int) -> int:
 
 def haq_fp8_linear(x, w_packed, w_scale, N: int, act: int = HAQ_ACT_NONE, *, out=None, workspace=None):
     """x fp16 or bf16 [T,K], weights of haq_quant_weight_fp8 packed with haq_pack_weight -> y [T,N] of x's type."""
-    T, K = x.shape
-    dtype = _rows16("haq_fp8_linear", x=x)
-    _fp8_weights("haq_fp8_linear", w_packed, w_scale, K, N)
-    y = out if out is not None else torch.empty((T, N), dtype=x.dtype, device=x.device)
-    if y.shape != (T, N) or _rows16("haq_fp8_linear", out=y) != dtype:
-        raise HaqError(f"haq_fp8_linear: out is {y.dtype} {tuple(y.shape)}, not {x.dtype} {(T, N)}")
+    name = "haq_fp8_linear"
+    (T, K), dtype, number, dev, ldx = _first_rows(name, x)
+    n = -(-K // 64) * 64 * (-(-N // 256) * 256)
+    if (w_packed.numel() < n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
+            or not _fits(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
+        _fp8_weights(name, w_packed, w_scale, K, N)
+    y, ldy = _out_rows(name, out, T, N, dtype, dev, x.device)
     if workspace is None:
         workspace = _ws(haq_fp8_linear_workspace_bytes(T, K, N), x.device)
-    _check(lib().haq_fp8_linear(_adr(x), _ld(x), dtype, _adr(w_packed), _adr(w_scale), T, K, N, act, _adr(y), _ld(y),
-                                _adr(workspace), workspace.numel() * workspace.element_size(), _stream_adr()))
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _flat(name, "workspace", workspace, workspace.dtype, 1)
+    _check(lib().haq_fp8_linear(x.data_ptr(), ldx, number, w_packed.data_ptr(), w_scale.data_ptr(), T, K, N, act, y.data_ptr(), ldy,
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(dev)))
     return y
 
 
@@ -416,26 +462,32 @@ def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, res
     """x fp16 or bf16 [T,K] (+ residual) -> (y, sum, q_packed, scale), None for what was not asked for: y is computed if it is
     given or no codes are asked for, the sum whenever there is a residual; codes HAQ_CODES_I8 (flat int8, scale [T]) or HAQ_CODES_E4M3
     (flat float8_e4m3fn, scale flat [ceil(K/128)][R]) in the packed operand layout."""
-    T, K = x.shape
-    dev = x.device
-    if residual is not None and sum_out is None:
-        sum_out = torch.empty((T, K), dtype=x.dtype, device=dev)
+    name = "haq_rmsnorm_quant"
+    shape, dtype, number, dev, ldx = _first_rows(name, x)
+    T, K = shape
+    pr = ldr = ps = lds = py = ldy = pq = pscale = 0
+    if residual is not None:
+        if sum_out is None:
+            sum_out = torch.empty(shape, dtype=dtype, device=x.device)
+        ldr, pr = _ld_like(residual, dtype, shape, dev), residual.data_ptr()
+    if sum_out is not None:
+        lds, ps = _ld_like(sum_out, dtype, shape, dev), sum_out.data_ptr()
     if y is None and codes == HAQ_CODES_NONE:
-        y = torch.empty((T, K), dtype=x.dtype, device=dev)
-    dtype = _rows16("haq_rmsnorm_quant", x=x, residual=residual, sum_out=sum_out, y=y)
-    _flat("haq_rmsnorm_quant", "weight", weight, torch.float32, K)
-    if codes in (HAQ_CODES_I8, HAQ_CODES_E4M3):
-        R = -(-T // 16) * 16 + 256
-        e4m3 = codes == HAQ_CODES_E4M3
-        n, n_scale, q_type = -(-K // 64) * 64 * R, _blocks(K) * R if e4m3 else T, torch.float8_e4m3fn if e4m3 else torch.int8
-        if q_packed is None:
-            q_packed = torch.empty((n,), dtype=q_type, device=dev)
-        if scale is None:
-            scale = torch.empty((n_scale,), dtype=torch.float32, device=dev)
-        _flat("haq_rmsnorm_quant", "q_packed", q_packed, q_type, n)
-        _flat("haq_rmsnorm_quant", "scale", scale, torch.float32, n_scale)
-    _check(lib().haq_rmsnorm_quant(_adr(x), _ld(x), _adr(residual), _ld(residual), _adr(weight), eps, dtype, T, K, _adr(sum_out),
-                                   _ld(sum_out), _adr(y), _ld(y), codes, _adr(q_packed), _adr(scale), _stream_adr()))
+        y = torch.empty(shape, dtype=dtype, device=x.device)
+    if y is not None:
+        ldy, py = _ld_like(y, dtype, shape, dev), y.data_ptr()
+    if ldr < 0 or lds < 0 or ldy < 0:
+        _rows16(name, x=x, residual=residual, sum_out=sum_out, y=y)
+    if not _fits(weight, torch.float32, K, dev):
+        _flat(name, "weight", weight, torch.float32, K)
+    if codes == HAQ_CODES_E4M3:
+        q_packed, scale = _codes_buffers(name, T, K, q_packed, scale, torch.float8_e4m3fn, -(-K // 128) * (-(-T // 16) * 16 + 256), dev, x)
+    elif codes == HAQ_CODES_I8:
+        q_packed, scale = _codes_buffers(name, T, K, q_packed, scale, torch.int8, T, dev, x)
+    if q_packed is not None:
+        pq, pscale = q_packed.data_ptr(), scale.data_ptr()
+    _check(lib().haq_rmsnorm_quant(x.data_ptr(), ldx, pr, ldr, weight.data_ptr(), eps, number, T, K, ps, lds, py, ldy, codes, pq, pscale,
+                                   _raw_stream(dev)))
     return y, sum_out, q_packed, scale
 
 

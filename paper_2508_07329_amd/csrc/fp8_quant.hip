@@ -11,10 +11,12 @@ constexpr int AQ_WAVES = 4;
 // of a block, whose maximum takes three lane exchanges, and with RW = 8 the codes of 8 rows fill the 128-byte lines of the
 // packed layout.  Bound: memory, two bytes read and one written an element.
 template <int DT, int RW>
-__global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a) {
+__global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a, int groups, int rows_x) {
     constexpr int LPR = 64 / RW;
     const int lane = threadIdx.x & 63;
-    const int row = (int)blockIdx.x * RW + lane / LPR, c = ((int)blockIdx.y * AQ_WAVES + (threadIdx.x >> 6)) * LPR + lane % LPR;
+    // work-group: AQ_WAVES pieces of a row group; `groups` of them to a row group, one behind the other, so that rows are read on
+    const int row = ((int)(blockIdx.x / groups) + (int)blockIdx.y * rows_x) * RW + lane / LPR;
+    const int c = ((int)(blockIdx.x % groups) * AQ_WAVES + (threadIdx.x >> 6)) * LPR + lane % LPR;
     const bool here = row < a.T && c < a.K / 16;
     float v[16] = {};
     if (here) {
@@ -32,8 +34,9 @@ __global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a
 
 template <int DT, int RW>
 int launch_act(const ActQuantArgs& a, hipStream_t st) {
-    const int pieces = cdiv(a.K / 16, 64 / RW);
-    hipLaunchKernelGGL((act_quant_kernel<DT, RW>), dim3(cdiv(a.T, RW), cdiv(pieces, AQ_WAVES)), dim3(AQ_WAVES * 64), 0, st, a);
+    const int groups = cdiv(cdiv(a.K / 16, 64 / RW), AQ_WAVES), row_groups = cdiv(a.T, RW);
+    const int most = (1 << 22) / groups, rows_x = row_groups < most ? row_groups : most;  // a grid has fewer than 2^32 threads in a direction
+    hipLaunchKernelGGL((act_quant_kernel<DT, RW>), dim3(rows_x * groups, cdiv(row_groups, rows_x)), dim3(AQ_WAVES * 64), 0, st, a, groups, rows_x);
     HAQ_CHECK_HIP(hipGetLastError());
     return HAQ_OK;
 }

@@ -43,10 +43,11 @@ __device__ __forceinline__ uint4 add16(const uint4& x, const uint4& r) {
     }
 }
 
-// A work-group holds RW rows; each of its waves 64 / RW chunks of 16 channels of all of them, a chunk to a lane, NB times.
-// RW = 8: the codes of 8 rows fill the 128-byte lines of the packed layout.
-template <int DT, int RW, int NB>
-__global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
+// A work-group holds RW rows; each of its waves 64 / RW chunks of 16 channels of all of them, a chunk to a lane, NB times; MAXW: its
+// most waves, which sets the register budget.  int8 keeps the normalised values across the reduction of the row maximum: normalising
+// twice reads the weight twice, which through a CU's load path costs as much as a row (8192 x 8192 64.5 -> 59.0 us).
+template <int DT, int RW, int NB, int MAXW, bool I8>
+__global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
     constexpr int LPR = 64 / RW;  // lanes of a wave that share a row
     __shared__ double sums[NORM_WAVES][RW];
     __shared__ float maxima[NORM_WAVES][RW];
@@ -119,8 +120,13 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
     for (int w = 0; w < nw; ++w) ss += sums[w][rl];
     const float inv = (float)(1.0 / sqrt(ss / (double)a.K + a.eps));
 
-    auto norm = [&](int b, float (&v)[16]) {
+    uint32_t top = 0;  // int8: largest magnitude, as bits, so that infinities and NaN (larger yet) show in it
+    float keep[I8 ? NB : 1][16];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
         const int c = chunk(b);
+        const bool here = live && c < nchunk;
+        float(&v)[16] = keep[I8 ? b : 0];
         unpack8<DT>(h[b][0], v);
         unpack8<DT>(h[b][1], v + 8);
         const float4* pg = reinterpret_cast<const float4*>(a.weight + (c < nchunk ? c : 0) * 16);
@@ -132,31 +138,25 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
             v[4 * i + 2] = (v[4 * i + 2] * inv) * g.z;
             v[4 * i + 3] = (v[4 * i + 3] * inv) * g.w;
         }
-    };
-    uint32_t top = 0;  // int8: largest magnitude, as bits, so that infinities and NaN (larger yet) show in it
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int c = chunk(b);
-        const bool here = live && c < nchunk;
-        float v[16];
-        norm(b, v);
         if (a.y && here) {
             uint4* p = reinterpret_cast<uint4*>((uint16_t*)a.y + r * a.ldy + c * 16);
             p[0] = pack8<DT>(v);
             p[1] = pack8<DT>(v + 8);
         }
-        if (a.codes == HAQ_CODES_E4M3) {
+        if (I8) {
+            if (here) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+            }
+        } else if (a.codes == HAQ_CODES_E4M3) {
             const BlockScale s = block_scale(max_of_8_lanes(here ? absmax16(v) : 0.0f));
             if (here) {
                 *reinterpret_cast<uint4*>(a.q + ((size_t)c * a.R + row) * 16) = e4m3x16(v, s.r);
                 if (c % 8 == 0) a.scale[(size_t)(c / 8) * a.R + row] = s.scale;
             }
-        } else if (a.codes == HAQ_CODES_I8 && here) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
         }
     }
-    if (a.codes != HAQ_CODES_I8) return;
+    if (!I8) return;
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     if (lane % LPR == 0) maxima[wave][rl] = __uint_as_float(top);
@@ -170,8 +170,7 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int c = chunk(b);
-        float v[16];
-        norm(b, v);
+        float(&v)[16] = keep[I8 ? b : 0];
         uint32_t w[4] = {0, 0, 0, 0};
         if (!zero) {
 #pragma unroll
@@ -183,28 +182,37 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void rmsnorm_kernel(NormArgs a) {
     }
 }
 
-template <int DT, int RW, int NB>
+template <int DT, int RW, int NB, int MAXW>
 int launch_one(const NormArgs& a, int waves, hipStream_t st) {
     const int groups = cdiv(a.T, RW), x = groups < MAX_GROUPS_X ? groups : MAX_GROUPS_X;
-    hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB>), dim3(x, cdiv(groups, x)), dim3(waves * 64), 0, st, a);
+    const dim3 grid(x, cdiv(groups, x)), block(waves * 64);
+    if (a.codes == HAQ_CODES_I8)
+        hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB, MAXW, true>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB, MAXW, false>), grid, block, 0, st, a);
     HAQ_CHECK_HIP(hipGetLastError());
     return HAQ_OK;
 }
 
-template <int DT, int RW>
-int launch_rows(const NormArgs& a, hipStream_t st) {
-    const int per_wave = 64 / RW, need = cdiv(a.K / 16, per_wave);  // wave-wide pieces of a row
-    if (need <= NORM_WAVES) return launch_one<DT, RW, 1>(a, need, st);
-    if (need <= 2 * NORM_WAVES) return launch_one<DT, RW, 2>(a, cdiv(need, 2), st);
-    if (need <= 4 * NORM_WAVES) return launch_one<DT, RW, 4>(a, cdiv(need, 4), st);
-    if constexpr (RW == 8) return launch_one<DT, RW, 8>(a, cdiv(need, 8), st);
-    return HAQ_ERR_UNSUPPORTED;
-}
-
+// One row to a work-group, or four (their codes are half of a 128-byte line of the packed layout), from 512 rows (two for each
+// CU) on and where there are codes to write.  us with one row / four:
+//   rows and the sum, no codes:  777 x 2064 5.3 / 5.5,  8192 x 8192 100 / 110
+//   with e4m3 codes:  1 x 4096 2.8 / 3.9,  64 x 4096 3.5 / 4.4,  256: 4.9 / 5.2,  512: 6.7 / 6.2,  2048: 20.8 / 17.4,  4096: 37.8 / 29.5,
+//                     4096 x 1024 11.8 / 9.7,  8192 x 8192 150 / 128,  2048 x 16384 71 / 61
+// Two rows lie between; eight, whole lines, gain up to 5 % at 4096 x 4096 and lose as much at 8192 x 8192, where they fill the registers.
 template <int DT>
 int launch_type(const NormArgs& a, hipStream_t st) {
-    if (a.K <= 16384 && a.T >= 8 * cu_count()) return launch_rows<DT, 8>(a, st);
-    return launch_rows<DT, 1>(a, st);
+    const int nchunk = a.K / 16;
+    if (a.codes != HAQ_CODES_NONE && a.T >= 2 * cu_count() && a.K <= 16384) {
+        const int need = cdiv(nchunk, 16);  // wave-wide pieces of four rows
+        if (need <= 8) return launch_one<DT, 4, 1, 8>(a, need, st);
+        if (need <= 16) return launch_one<DT, 4, 2, 8>(a, cdiv(need, 2), st);
+        if (need <= 32) return launch_one<DT, 4, 4, 8>(a, cdiv(need, 4), st);
+        return launch_one<DT, 4, 4, 16>(a, cdiv(need, 4), st);
+    }
+    const int need = cdiv(nchunk, 64);
+    if (need <= 16) return launch_one<DT, 1, 1, 16>(a, need, st);
+    return launch_one<DT, 1, 4, 16>(a, cdiv(need, 4), st);
 }
 
 }  // namespace
