@@ -192,7 +192,7 @@ int32_t haq_w8a8_linear_asym(const void* x_fp16, int64_t ldx, const float* s, co
  *
  * x and y are binary16 or bfloat16 by dtype (HAQ_F16, HAQ_BF16; both the same), rows
  * [T x K] and [T x N].  K % 16 == 0, K <= 65536, N % 16 == 0, T and N <= 2^24.  T == 0 is a
- * no-op.  y must not overlap an input.
+ * no-op.  y must not overlap an input, but for the rows x of haq_fp8_linear.
  *
  * haq_quant_weight_fp8 (offline): w fp32 [K x N] -> wq [K x N] codes, canonical layout,
  *   and w_scale; to be packed with haq_pack_weight like int8 codes (the layout is of bytes).

@@ -92,6 +92,7 @@ _CALLS = {
     "haq_moe_w8a8_ffn": (_P, _P, _L, _P, _L, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P, _P, _Z, _P),
     "haq_moe_w8a8_ffn_static": (_P, _L, _P, _L, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P),
     "haq_moe_w8a8_ffn_asym": (_P, _L, _P, _L, _P, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P, _P, _Z, _P),
+    "haq_quant_weight_fp8": (_P, _I, _I, _P, _P, _P),
     "haq_quant_act_fp8_packed": (_P, _L, _I, _I, _I, _P, _P, _P),
     "haq_gemm_fp8_packed": (_P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _L, _P),
     "haq_fp8_linear": (_P, _L, _I, _P, _P, _I, _I, _I, _I, _P, _L, _P, _Z, _P),
@@ -344,23 +345,22 @@ def _first_rows(name, x):
     return shape, dtype, number, dev, s[0] if shape[0] > 1 else shape[1]
 
 
-def _blocks(n: int) -> int:
-    return -(-n // 128)
-
-
 def haq_quant_weight_fp8(w, *, wq=None, w_scale=None):
     """w fp32 [K,N] -> (wq float8_e4m3fn [K,N] canonical, for haq_pack_weight; w_scale [ceil(K/128), ceil(N/128)])."""
+    name = "haq_quant_weight_fp8"
     K, N = w.shape
-    if w.dtype != torch.float32 or not w.is_contiguous():
-        raise HaqError(f"haq_quant_weight_fp8: w must be a contiguous fp32 matrix, got {w.dtype} with strides {tuple(w.stride())}")
-    _here("haq_quant_weight_fp8", "w", w)
+    dev, blocks = w.get_device(), (-(-K // 128), -(-N // 128))
+    if dev < 0 or dev != _current_device() or not _fits(w, torch.float32, 0, dev):
+        _flat(name, "w", w, torch.float32, K * N)
     if wq is None:
         wq = torch.empty((K, N), dtype=torch.float8_e4m3fn, device=w.device)
+    elif not _fits(wq, torch.float8_e4m3fn, K * N, dev):
+        _flat(name, "wq", wq, torch.float8_e4m3fn, K * N)
     if w_scale is None:
-        w_scale = torch.empty((_blocks(K), _blocks(N)), dtype=torch.float32, device=w.device)
-    _flat("haq_quant_weight_fp8", "wq", wq, torch.float8_e4m3fn, K * N)
-    _flat("haq_quant_weight_fp8", "w_scale", w_scale, torch.float32, _blocks(K) * _blocks(N))
-    _check(lib().haq_quant_weight_fp8(_ptr(w), K, N, _ptr(wq), _ptr(w_scale), _stream()))
+        w_scale = torch.empty(blocks, dtype=torch.float32, device=w.device)
+    elif not _fits(w_scale, torch.float32, blocks[0] * blocks[1], dev):
+        _flat(name, "w_scale", w_scale, torch.float32, blocks[0] * blocks[1])
+    _check(lib().haq_quant_weight_fp8(w.data_ptr(), K, N, wq.data_ptr(), w_scale.data_ptr(), _raw_stream(dev)))
     return wq, w_scale
 
 
@@ -368,9 +368,8 @@ def haq_act_scales_fp8_bytes(T: int, K: int) -> int:
     return int(lib().haq_act_scales_fp8_bytes(T, K))
 
 
-def _codes_buffers(name, T, K, q, scale, q_type, n_scale, dev, x):
+def _codes_buffers(name, n, q, scale, q_type, n_scale, dev, x):
     """The packed codes' buffer and their scales', made or looked over."""
-    n = -(-K // 64) * 64 * (-(-T // 16) * 16 + 256)
     if q is None:
         q = torch.empty((n,), dtype=q_type, device=x.device)
     elif not _fits(q, q_type, n, dev):
@@ -385,8 +384,9 @@ def _codes_buffers(name, T, K, q, scale, q_type, n_scale, dev, x):
 def haq_quant_act_fp8_packed(x, *, q_packed=None, block_scale=None):
     """x fp16 or bf16 [T,K] -> (codes in the packed operand layout (flat float8_e4m3fn), block_scale (flat fp32, [ceil(K/128)][R]))."""
     (T, K), _, number, dev, ld = _first_rows("haq_quant_act_fp8_packed", x)
-    q, scale = _codes_buffers("haq_quant_act_fp8_packed", T, K, q_packed, block_scale, torch.float8_e4m3fn,
-                              -(-K // 128) * (-(-T // 16) * 16 + 256), dev, x)
+    R = -(-T // 16) * 16 + 256
+    q, scale = _codes_buffers("haq_quant_act_fp8_packed", -(-K // 64) * 64 * R, q_packed, block_scale, torch.float8_e4m3fn, -(-K // 128) * R,
+                              dev, x)
     _check(lib().haq_quant_act_fp8_packed(x.data_ptr(), ld, number, T, K, q.data_ptr(), scale.data_ptr(), _raw_stream(dev)))
     return q, scale
 
@@ -399,7 +399,7 @@ def _fp8_weights(name, w_packed, w_scale, K, N):
     if w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.numel() < n:
         raise HaqError(f"{name}: w_packed must hold {n} bytes from haq_pack_weight, got {w_packed.dtype} {tuple(w_packed.shape)}")
     _here(name, "w_packed", w_packed)
-    _flat(name, "w_scale", w_scale, torch.float32, _blocks(K) * _blocks(N))
+    _flat(name, "w_scale", w_scale, torch.float32, -(-K // 128) * -(-N // 128))
 
 
 def _out_rows(name, out, T, N, dtype, dev, device):
@@ -480,12 +480,13 @@ def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, res
         _rows16(name, x=x, residual=residual, sum_out=sum_out, y=y)
     if not _fits(weight, torch.float32, K, dev):
         _flat(name, "weight", weight, torch.float32, K)
-    if codes == HAQ_CODES_E4M3:
-        q_packed, scale = _codes_buffers(name, T, K, q_packed, scale, torch.float8_e4m3fn, -(-K // 128) * (-(-T // 16) * 16 + 256), dev, x)
-    elif codes == HAQ_CODES_I8:
-        q_packed, scale = _codes_buffers(name, T, K, q_packed, scale, torch.int8, T, dev, x)
-    if q_packed is not None:
+    if codes:
+        R = -(-T // 16) * 16 + 256
+        q_type, n_scale = (torch.int8, T) if codes == HAQ_CODES_I8 else (torch.float8_e4m3fn, -(-K // 128) * R)
+        q_packed, scale = _codes_buffers(name, -(-K // 64) * 64 * R, q_packed, scale, q_type, n_scale, dev, x)
         pq, pscale = q_packed.data_ptr(), scale.data_ptr()
+    else:
+        q_packed = scale = None
     _check(lib().haq_rmsnorm_quant(x.data_ptr(), ldx, pr, ldr, weight.data_ptr(), eps, number, T, K, ps, lds, py, ldy, codes, pq, pscale,
                                    _raw_stream(dev)))
     return y, sum_out, q_packed, scale

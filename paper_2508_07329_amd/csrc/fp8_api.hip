@@ -106,7 +106,9 @@ int32_t haq_fp8_linear(const void* x, int64_t ldx, int32_t dtype, const uint8_t*
     uint8_t* q = (uint8_t*)workspace;
     float* sa = (float*)(q + scales_at(T, K));
     const Fp8GemmArgs a = gemm_args(q, sa, w_packed, w_scale, T, K, N, act, y, ldy);
-    if (fp8_stream_rows16_fits(T, K)) return launch_fp8_stream_rows16(a, x, ldx, dtype, (hipStream_t)stream);
+    // In the one launch some work-groups read x while others store y: not where the two overlap (their rows may lie side by side).
+    const uintptr_t xb = (uintptr_t)x, xe = xb + ((size_t)(T - 1) * ldx + K) * 2, yb = (uintptr_t)y, ye = yb + ((size_t)(T - 1) * ldy + N) * 2;
+    if (fp8_stream_rows16_fits(T, K) && (xe <= yb || ye <= xb)) return launch_fp8_stream_rows16(a, x, ldx, dtype, (hipStream_t)stream);
     if (const int rc = launch_act_quant_fp8({x, ldx, T, K, q, act_rows(T), sa}, dtype, (hipStream_t)stream)) return rc;
     return launch_fp8_gemm(a, dtype, (hipStream_t)stream);
 }

@@ -60,12 +60,13 @@ int main() {
     char what;
     int a, b, c;
     uint8_t* u = (uint8_t*)256;  // addresses that nothing follows
+    uint8_t* far = (uint8_t*)((uintptr_t)1 << 46);
     float* f = (float*)256;
     while (scanf(" %c %d %d %d", &what, &a, &b, &c) == 4) {
         int rc = HAQ_OK;
         switch (what) {
             case 'g': rc = haq_gemm_fp8_packed(u, f, u, f, a, b, c, HAQ_ACT_NONE, HAQ_F16, u, c, nullptr); break;
-            case 'l': rc = haq_fp8_linear(u, b, HAQ_F16, u, f, a, b, c, HAQ_ACT_NONE, u, c, u, (size_t)1 << 46, nullptr); break;
+            case 'l': rc = haq_fp8_linear(u, b, HAQ_F16, u, f, a, b, c, HAQ_ACT_NONE, far, c, u, (size_t)1 << 46, nullptr); break;
             case 'q': rc = haq_quant_act_fp8_packed(u, b, c, a, b, u, f, nullptr); break;
             case 'n': rc = haq_rmsnorm_quant(u, b, u, b, f, 1e-5, HAQ_BF16, a, b, u, b, u, b, c, c ? u : nullptr, c ? f : nullptr, nullptr); break;
             case 'w': rc = haq_quant_weight_fp8(f, a, b, u, f, nullptr); break;

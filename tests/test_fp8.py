@@ -176,6 +176,62 @@ def test_linear_overflows_to_infinity_in_binary16_only():
         assert bool(y.isinf().all()) == (dtype == F16)
 
 
+@pytest.mark.parametrize("T", [3, 40])
+def test_linear_into_the_buffer_of_its_rows(T):
+    """y over x, and beside it in one matrix."""
+    K, N = 528, 400
+    x = ref.rows(T, T, K, F16)
+    wq, sw, wp, swd = weights(9, K, N)
+    want, bound = ref.linear(*ref.act_codes(x.float()), wq, sw)
+    both = torch.zeros((T, K + N), dtype=F16, device=DEV)
+    both[:, :K] = x.to(DEV)
+    haq.haq_fp8_linear(both[:, :K], wp, swd, N, out=both[:, K:])
+    ref.assert_linear(both[:, K:].cpu(), want, bound)
+    assert same_bits(both[:, :K], x)
+    over = x.to(DEV)
+    haq.haq_fp8_linear(over, wp, swd, N, out=over[:, :N])
+    ref.assert_linear(over[:, :N].cpu(), want, bound)
+    assert same_bits(over[:, N:], x[:, N:])
+
+
+def test_offsets_past_32_bits():
+    """Codes, weights and rows of 4 GB and more: the first and the last rows and channels."""
+    K, many = 1040, 4_200_016
+    x = ref.rows(1, 64, K, F16)
+    last = torch.cat([torch.arange(32), many - 32 + torch.arange(32)])
+    big = torch.zeros((many, K), dtype=F16, device=DEV)
+    big[last.to(DEV)] = x.to(DEV)
+    wq, sw, wp, swd = weights(3, K, 32)
+    y = haq.haq_fp8_linear(big, wp, swd, 32)
+    ref.assert_linear(y[last.to(DEV)].cpu(), *ref.linear(*ref.act_codes(x.float()), wq, sw))
+    assert not y[32:-32].any()
+    del y
+    n, _, q, s = haq.haq_rmsnorm_quant(big, torch.ones(K, device=DEV), EPS, haq.HAQ_CODES_E4M3, y=torch.empty_like(big))
+    _, v = ref.norm(x, torch.ones(K), EPS)
+    assert same_bits(n[last.to(DEV)], v.to(F16))
+    R = ref.padded_rows(many)
+    got = q.view(torch.uint8).view(-1, R, 16)[: K // 16][:, last.to(DEV)].permute(1, 0, 2).reshape(64, K)
+    assert same_codes(got, ref.act_codes(v)[0])
+    del n, q, s, big
+    w = torch.zeros((K, many), device=DEV)
+    small = torch.randn(K, 512, generator=torch.Generator().manual_seed(5)) * 0.02
+    at = many // 128 * 128 - 128  # the last whole block and what is behind it
+    w[:, :128], w[:, at:] = small[:, :128].to(DEV), small[:, 128:128 + many - at].to(DEV)
+    wq, sw = haq.haq_quant_weight_fp8(w)
+    del w
+    wp = haq.haq_pack_weight(wq)
+    keep = torch.cat([wq[:, :128].cpu().view(torch.uint8), wq[:, at:].cpu().view(torch.uint8)], dim=1)
+    want_q, _ = ref.weight_codes(small[:, : 128 + many - at])
+    assert same_codes(keep, want_q)
+    scales = torch.cat([sw[:, :1], sw[:, at // 128:]], dim=1).cpu()
+    del wq
+    for T in (5, 40):
+        x = ref.rows(T, T, K, F16)
+        y = haq.haq_fp8_linear(x.to(DEV), wp, sw, many)
+        want, bound = ref.linear(*ref.act_codes(x.float()), want_q, scales)
+        ref.assert_linear(torch.cat([y[:, :128], y[:, at:]], dim=1).cpu(), want, bound)
+
+
 def test_no_tokens():
     _, _, wp, sw = weights(1, 128, 32)
     x = torch.empty(0, 128, dtype=F16, device=DEV)

@@ -26,10 +26,7 @@ POINTERS = ("x", "residual", "weight", "sum", "y", "q", "scale", "w", "wq", "w_s
 def call(name, **changes):
     """The entry point on arguments that are in order but for `changes`."""
     assert set(changes) <= set(ORDER[name])
-    args = {**ORDER[name], **changes}
-    if name == "haq_quant_weight_fp8":  # no argument types of its own
-        args = {k: C.c_void_p(v) if k in POINTERS + ("stream",) else v for k, v in args.items()}
-    return getattr(haq.lib(), name)(*args.values())
+    return getattr(haq.lib(), name)(*{**ORDER[name], **changes}.values())
 
 
 COMMON = [("dtype", 2, UNSUPPORTED), ("dtype", -1, UNSUPPORTED), ("T", -1, BAD_ARG), ("T", (1 << 24) + 1, UNSUPPORTED), ("K", 0, BAD_ARG), ("K", 264, UNSUPPORTED),
