@@ -40,18 +40,14 @@ __device__ __forceinline__ void fp8_to_lds4(Fp8Rsrc, int8_t*, uint32_t) {}
 #endif
 constexpr uint32_t FP8_PAST_END = 0xFFFF0000u;  // an offset past every resource's bytes
 
-// Work-group id -> tile: ids go round-robin to the 8 XCDs; each of them (one L2) takes a contiguous range of tiles, in bands
-// of row tiles (1024 rows), rows fastest inside a band, so that what an XCD holds at a time shares rows and channels.
+// Tile number -> tile, in bands of row tiles (1024 rows), rows fastest inside a band, so that neighbours share rows and channels.
 template <int BM, int BN>
-__device__ __forceinline__ bool fp8_tile(const Fp8GemmArgs& a, int& m0, int& n0) {
+__device__ __forceinline__ void fp8_tile(const Fp8GemmArgs& a, int id, int& m0, int& n0) {
     constexpr int BAND = 1024 / BM;
-    const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN, total = mt * nt, per = (total + 7) / 8;
-    const int slot = blockIdx.x / 8, id = (int)(blockIdx.x % 8) * per + slot;
-    if (slot >= per || id >= total) return false;
+    const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
     const int band = id / (BAND * nt), rem = id % (BAND * nt), rows = min(BAND, mt - band * BAND);
     m0 = (band * BAND + rem % rows) * BM;
     n0 = rem / rows * BN;
-    return true;
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG>
@@ -61,9 +57,10 @@ struct Fp8Shape {
     static constexpr int LDS_BYTES = KG * STAGES * STAGE_BYTES;
 };
 
-// KG: groups of waves that share the tile and take its K-steps in turn, each with a ring of its own; their sums are added at the end.
-template <int DT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG, int MINB>
-__global__ __launch_bounds__(KG * WAVES_M * WAVES_N * 64, MINB) void fp8_gemm_kernel(Fp8GemmArgs a) {
+// One tile by a whole work-group.  KG: groups of waves that share the tile and take its K-steps in turn, each with a ring of its own;
+// their sums are added at the end.
+template <int DT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG>
+__device__ __forceinline__ void fp8_gemm_tile(const Fp8GemmArgs& a, const int m0, const int n0, int8_t* all_lds) {
     using S = Fp8Shape<BM, BN, WAVES_M, WAVES_N, STAGES, KG>;
     constexpr int NW = S::NW, STAGE = S::STAGE_BYTES;
     constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, MI = WM / 16, NJ = WN / 16, NP = NJ / 2;
@@ -78,10 +75,6 @@ __global__ __launch_bounds__(KG * WAVES_M * WAVES_N * 64, MINB) void fp8_gemm_ke
     constexpr int EXCHANGE = KG == 2 ? BM * BN * 4 : 0;
     static_assert(KG == 1 || (KG == 2 && MI % 2 == 0), "two groups store half of the rows each");
     static_assert(EXCHANGE + KG * NW * 16 * PITCH <= S::LDS_BYTES, "epilogue staging");
-    extern __shared__ __attribute__((aligned(1024))) int8_t all_lds[];
-
-    int m0, n0;
-    if (!fp8_tile<BM, BN>(a, m0, n0)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = KG == 1 ? 0 : wave_id / NW, wave = KG == 1 ? wave_id : wave_id % NW;
     int8_t* lds = all_lds + kg * STAGES * STAGE;
@@ -285,6 +278,40 @@ __global__ __launch_bounds__(KG * WAVES_M * WAVES_N * 64, MINB) void fp8_gemm_ke
             if (row < a.M && col < a.N) *reinterpret_cast<uint4*>((uint16_t*)a.Y + (size_t)row * a.ldy + col) = make_uint4(v0.x, v0.y, v1.x, v1.y);
         }
         HAQ_FP8_FENCE();
+    }
+}
+
+// Work-group ids go round-robin to the 8 XCDs, each of which (one L2) takes a contiguous range of the tiles.
+template <int DT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int KG, int MINB>
+__global__ __launch_bounds__(KG * WAVES_M * WAVES_N * 64, MINB) void fp8_gemm_kernel(Fp8GemmArgs a, int tiles) {
+    extern __shared__ __attribute__((aligned(1024))) int8_t all_lds[];
+    const int per = (tiles + 7) / 8, xcd = blockIdx.x % 8, slot = blockIdx.x / 8, id = xcd * per + slot;
+    if (slot >= per || id >= tiles) return;
+    int m0, n0;
+    fp8_tile<BM, BN>(a, id, m0, n0);
+    fp8_gemm_tile<DT, BM, BN, WAVES_M, WAVES_N, STAGES, KG>(a, m0, n0, all_lds);
+}
+
+// 256 x 256 tiles, the last ones (behind `whole`) in halves of 256 x 128: where those fill the last round of work-groups, it takes some
+// 0.6 of the time of one of whole tiles that half of the CUs hold.  Every XCD takes its share of both, halves last.  Weights cold, us,
+// whole tiles only / with halves: 4096 x 4096 x 14336 218 / 195, 4096 x 2048 x 4352 51.2 / 44.6, 2304 x 4096 x 8192 91.0 / 78.7.
+// (256 x 128 tiles in halves of 128 x 128 were the fastest at 2 of 150 sizes, by 1 %.)
+template <int DT>
+__global__ __launch_bounds__(512, 2) void fp8_gemm_halves_kernel(Fp8GemmArgs a, int whole, int tiles) {
+    extern __shared__ __attribute__((aligned(1024))) int8_t all_lds[];
+    const int halves = 2 * (tiles - whole), per_w = (whole + 7) / 8, per_h = (halves + 7) / 8, xcd = blockIdx.x % 8, slot = blockIdx.x / 8;
+    int m0, n0;
+    if (slot < per_w) {
+        const int id = xcd * per_w + slot;
+        if (id >= whole) return;
+        fp8_tile<256, 256>(a, id, m0, n0);
+        fp8_gemm_tile<DT, 256, 256, 4, 2, 2, 1>(a, m0, n0, all_lds);
+    } else {
+        const int id = xcd * per_h + slot - per_w;
+        if (slot - per_w >= per_h || id >= halves) return;
+        fp8_tile<256, 256>(a, whole + id / 2, m0, n0);
+        n0 += id % 2 * 128;
+        if (n0 < a.N) fp8_gemm_tile<DT, 256, 128, 4, 2, 2, 1>(a, m0, n0, all_lds);
     }
 }
 

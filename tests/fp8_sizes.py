@@ -20,3 +20,6 @@ TILED = {
     (256, 128, 1): [(257, 16, 13168), (257, 256, 13072), (257, 400, 13072)],
     (256, 256, 1): [(513, 16, 14608), (513, 128, 14576), (513, 256, 14576), (513, 336, 14576)],
 }
+# 256 x 256 tiles of which those behind whole rounds are taken in halves: 10 of them, of 16 channels (the second halves hold none) and of
+# 144; one; many
+HALVES = [(2049, 272, 14608), (2049, 144, 14480), (2049, 400, 14576), (1281, 1168, 11920)]

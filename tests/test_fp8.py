@@ -4,7 +4,7 @@ import torch
 
 import paper_2508_07329_amd as haq
 from tests import fp8_reference as ref
-from tests.fp8_sizes import STREAM, TILED
+from tests.fp8_sizes import HALVES, STREAM, TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -117,7 +117,7 @@ def test_linear(T, K, N, dtype):
     assert same_bits(y, haq.haq_fp8_linear(x.to(DEV), wp, swd, N, act))  # a call repeated is the same
 
 
-@pytest.mark.parametrize("T,K,N", [size for shapes in (STREAM, TILED) for sizes in shapes.values() for size in sizes])
+@pytest.mark.parametrize("T,K,N", [size for shapes in (STREAM, TILED) for sizes in shapes.values() for size in sizes] + HALVES)
 def test_linear_on_each_kernel(T, K, N):
     x = ref.rows(T * K + N, T, K, F16)
     wq, sw, wp, swd = weights(T + K + N, K, N)

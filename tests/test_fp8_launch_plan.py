@@ -8,7 +8,7 @@ import subprocess
 import pytest
 
 from paper_2508_07329_amd import build as hip_build
-from tests.fp8_sizes import STREAM, TILED
+from tests.fp8_sizes import HALVES, STREAM, TILED
 from tests.test_launch_plan import HERE, _host_program
 
 MOST_ROWS = 1 << 24
@@ -31,7 +31,7 @@ def plan(tmp_path_factory):
                 launches = []
                 continue
             name, gx, gy, threads, lds = line.split()
-            kernel = re.search(r"(fp8_gemm|fp8_stream|act_quant|weight_quant|rmsnorm)_kernel", name).group(1)
+            kernel = re.search(r"(fp8_gemm_halves|fp8_gemm|fp8_stream|act_quant|weight_quant|rmsnorm)_kernel", name).group(1)
             launches.append((kernel, [int(v) for v in re.findall(r"L[ib](\d+)E", name)], (int(gx), int(gy)), int(threads), int(lds)))
         assert len(res) == len(calls)
         return res
@@ -48,10 +48,14 @@ def fits_the_machine(launch):
     return gx * threads < 1 << 32 and gy < 1 << 16 and 64 <= threads <= 1024 and lds <= 160 * 1024
 
 
-def work_groups(kernel, t, M, N):
+def work_groups(kernel, t, M, N, n_cu):
     """What the grid has to reach."""
     if kernel == "fp8_gemm":
         return cd(M, t[1]) * cd(N, t[2])
+    if kernel == "fp8_gemm_halves":  # whole rounds of tiles, and at most one of halves; every XCD a share of both
+        tiles = cd(M, 256) * cd(N, 256)
+        assert tiles > n_cu and 0 < 2 * (tiles % n_cu) <= n_cu
+        return cd(tiles - tiles % n_cu, 8) * 8 + cd(2 * (tiles % n_cu), 8) * 8
     assert kernel == "fp8_stream"
     return (cd(M, 16 * t[2]) if t[7] else 1) * cd(N, 16 * t[1])
 
@@ -66,8 +70,10 @@ def test_every_tile_of_a_linear_has_a_work_group(plan):
         for (M, K, N), launches in zip(sizes, plan(calls)[1:]):
             (kernel, t, grid, threads, lds), = launches
             assert fits_the_machine(launches[0]), (M, K, N, launches)
-            assert grid[0] * grid[1] >= work_groups(kernel, t, M, N), (M, K, N, launches)
-            if kernel == "fp8_gemm":
+            assert grid[0] * grid[1] >= work_groups(kernel, t, M, N, n_cu), (M, K, N, launches)
+            if kernel == "fp8_gemm_halves":
+                assert grid[0] % 8 == 0 and threads == 512 and lds == 2 * (512 * 128 + 8 * 256)
+            elif kernel == "fp8_gemm":
                 assert grid[0] % 8 == 0 and threads == 64 * t[3] * t[4] * t[6] and lds == t[6] * t[5] * ((t[1] + t[2]) * 128 + t[3] * t[4] * 256)
             else:
                 assert t[6] == 0 and (t[7] == 1 or M <= 16 * t[2]) and threads == 64 * t[3] and lds == t[3] * t[1] * t[2] * 1024
@@ -82,6 +88,14 @@ def test_sizes_of_the_gpu_tests_take_the_kernels_that_they_are_for(plan):
         for s, launches in zip(sizes, plan([("g", *s) for s in sizes])):
             (kernel, t, *_), = launches
             assert kernel == "fp8_gemm" and (t[1], t[2], t[6]) == shape, (s, shape, launches)
+
+
+def test_halves_of_the_last_tiles(plan):
+    """Where the tiles behind whole rounds fill at most half of one."""
+    halves = HALVES + [(4096, 4096, 14336), (2304, 4096, 8192), (4096, 2048, 4352)]
+    whole = [(4096, 4096, 4096), (8192, 8192, 8192), (3000, 4096, 14336)]
+    of = lambda sizes: {launches[0][0] for launches in plan([("g", *s) for s in sizes])}
+    assert of(halves) == {"fp8_gemm_halves"} and of(whole) == {"fp8_gemm"}
 
 
 def test_a_few_rows_take_one_launch_and_more_two(plan):
