@@ -52,7 +52,14 @@ __global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
     __shared__ double sums[NORM_WAVES][RW];
     __shared__ float maxima[NORM_WAVES][RW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    const int rl = lane / LPR, row = (int)(blockIdx.y * gridDim.x + blockIdx.x) * RW + rl;
+    int group = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+    if (a.codes) {  // ids go round-robin to the 8 XCDs: the work-groups whose codes share lines go to one of them, whose L2 fills the lines
+        constexpr int LINE = 8 / RW;
+        const int in = group % (8 * LINE);
+        group += (in % 8) * LINE + in / 8 - in;
+        if (group * RW >= a.T) return;  // the grid is in whole lines
+    }
+    const int rl = lane / LPR, row = group * RW + rl;
     const int nchunk = a.K / 16;
     const bool live = row < a.T;
     const size_t r = live ? row : 0;
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
 
 template <int DT, int RW, int NB, int MAXW>
 int launch_one(const NormArgs& a, int waves, hipStream_t st) {
-    const int groups = cdiv(a.T, RW), x = groups < MAX_GROUPS_X ? groups : MAX_GROUPS_X;
+    const int groups = a.codes ? (int)round_up(cdiv(a.T, RW), 64 / RW) : cdiv(a.T, RW), x = groups < MAX_GROUPS_X ? groups : MAX_GROUPS_X;
     const dim3 grid(x, cdiv(groups, x)), block(waves * 64);
     if (a.codes == HAQ_CODES_I8)
         hipLaunchKernelGGL((rmsnorm_kernel<DT, RW, NB, MAXW, true>), grid, block, 0, st, a);
@@ -194,23 +201,30 @@ int launch_one(const NormArgs& a, int waves, hipStream_t st) {
     return HAQ_OK;
 }
 
-// One row to a work-group, or four (their codes are half of a 128-byte line of the packed layout), from 512 rows (two for each
-// CU) on and where there are codes to write.  us with one row / four:
-//   rows and the sum, no codes:  777 x 2064 5.3 / 5.5,  8192 x 8192 100 / 110
-//   with e4m3 codes:  1 x 4096 2.8 / 3.9,  64 x 4096 3.5 / 4.4,  256: 4.9 / 5.2,  512: 6.7 / 6.2,  2048: 20.8 / 17.4,  4096: 37.8 / 29.5,
-//                     4096 x 1024 11.8 / 9.7,  8192 x 8192 150 / 128,  2048 x 16384 71 / 61
-// Two rows lie between; eight, whole lines, gain up to 5 % at 4096 x 4096 and lose as much at 8192 x 8192, where they fill the registers.
+template <int DT, int RW>
+int launch_rows(const NormArgs& a, hipStream_t st) {
+    const int need = cdiv(a.K / 16, 64 / RW);  // wave-wide pieces of RW rows
+    if (need <= 8) return launch_one<DT, RW, 1, 8>(a, need, st);
+    if (need <= 16) return launch_one<DT, RW, 2, 8>(a, cdiv(need, 2), st);
+    if (need <= 32) return launch_one<DT, RW, 4, 8>(a, cdiv(need, 4), st);
+    return launch_one<DT, RW, 4, 16>(a, cdiv(need, 4), st);
+}
+
+// One row to a work-group; where there are codes to write, two from 512 rows (two for each CU) on and four from 2048, up to K = 16384.
+// us with one row / two / four:
+//   rows and the sum, no codes:  777 x 2064 5.3 / 5.4 / 5.5,  8192 x 8192 100 / 102 / 110
+//   with e4m3 codes:  1 x 4096 2.8 / 3.2 / 3.9,  64: 3.5 / 3.8 / 4.4;  700 x 2048 4.8 / 4.8 / 5.0,  1024 x 8192 18.6 / 16.4 / 17.7,  1500 x 6144 20.9 / 19.2 / 19.7
+//                     2048 x 4096 18.3 / 16.9 / 16.9,  8000 x 1040 19.5 / 17.6 / 17.5,  8192 x 8192 127 / 117 / 104
+//   with int8 codes:  512 x 8192 11.1 / 11.6 / 14.4,  1024 x 4096 10.8 / 10.6 / 11.6,  4096 x 8192 58.3 / 56.3 / 57.8,  6000 x 2048 31.2 / 28.8 / 27.9
+// Eight rows, whole lines without the help of the L2, gain up to 5 % at 4096 x 4096 and lose as much at 8192 x 8192, where they fill
+// the registers.  (The work-groups of a line's rows on different XCDs: 256 x 4096 4.9 against 4.3, 8192 x 8192 109 against 104.)
 template <int DT>
 int launch_type(const NormArgs& a, hipStream_t st) {
-    const int nchunk = a.K / 16;
-    if (a.codes != HAQ_CODES_NONE && a.T >= 2 * cu_count() && a.K <= 16384) {
-        const int need = cdiv(nchunk, 16);  // wave-wide pieces of four rows
-        if (need <= 8) return launch_one<DT, 4, 1, 8>(a, need, st);
-        if (need <= 16) return launch_one<DT, 4, 2, 8>(a, cdiv(need, 2), st);
-        if (need <= 32) return launch_one<DT, 4, 4, 8>(a, cdiv(need, 4), st);
-        return launch_one<DT, 4, 4, 16>(a, cdiv(need, 4), st);
+    if (a.codes != HAQ_CODES_NONE && a.K <= 16384) {
+        if (a.T >= 8 * cu_count()) return launch_rows<DT, 4>(a, st);
+        if (a.T >= 2 * cu_count()) return launch_rows<DT, 2>(a, st);
     }
-    const int need = cdiv(nchunk, 64);
+    const int need = cdiv(a.K / 16, 64);
     if (need <= 16) return launch_one<DT, 1, 1, 16>(a, need, st);
     return launch_one<DT, 1, 4, 16>(a, cdiv(need, 4), st);
 }

@@ -259,8 +259,8 @@ def check_norm(x, weight, residual, codes, want_y, eps=EPS, **buffers):
     return v
 
 
-@pytest.mark.parametrize("T,K", [(1, 16), (1, 4096), (2, 144), (3, 16384), (1, 65536), (2, 20496), (7, 1040), (33, 2064), (300, 272), (2049, 1024),
-                                 (2050, 208), (2048, 4112), (2051, 8208)])
+@pytest.mark.parametrize("T,K", [(1, 16), (1, 4096), (2, 144), (3, 16384), (1, 65536), (2, 20496), (7, 1040), (33, 2064), (300, 272), (513, 272), (2046, 1040),
+                                 (1000, 8208), (2049, 1024), (2050, 208), (2048, 4112), (2051, 8208)])
 @pytest.mark.parametrize("codes", [haq.HAQ_CODES_NONE, haq.HAQ_CODES_I8, haq.HAQ_CODES_E4M3])
 def test_norm(T, K, codes):
     for dtype in (F16, BF16):
@@ -270,7 +270,7 @@ def test_norm(T, K, codes):
     check_norm(x, weight, None, codes, codes == haq.HAQ_CODES_NONE)
 
 
-@pytest.mark.parametrize("T", [4, 2100])
+@pytest.mark.parametrize("T", [4, 700, 2100])
 @pytest.mark.parametrize("codes", [haq.HAQ_CODES_NONE, haq.HAQ_CODES_I8, haq.HAQ_CODES_E4M3])
 def test_norm_of_extreme_rows(T, codes):
     """Rows of zeros, of subnormals, of values whose squares overflow binary32, weights of zero and huge ones."""
@@ -285,7 +285,7 @@ def test_norm_of_extreme_rows(T, codes):
     check_norm(x, weight, None, codes, True, eps=1e-30)
 
 
-@pytest.mark.parametrize("T", [5, 2100])
+@pytest.mark.parametrize("T", [5, 700, 2100])
 def test_norm_rows_with_infinities_and_nan_stay_apart(T):
     K = 272
     x = ref.rows(4, T, K, F16)
@@ -307,7 +307,7 @@ def test_norm_rows_with_infinities_and_nan_stay_apart(T):
             assert bool(((ref.unpack_act(q.cpu(), T, K)[[1, 3, 4]] & 0x7F) == 0x7F).any(dim=1).all())
 
 
-@pytest.mark.parametrize("T,K", [(3, 400), (2100, 400)])
+@pytest.mark.parametrize("T,K", [(3, 400), (701, 400), (2100, 400)])
 def test_norm_in_place_and_with_gaps_between_rows(T, K):
     x, r = ref.rows(1, T, K, F16), ref.rows(2, T, K, F16)
     weight = 1.0 + 0.1 * torch.randn(K, generator=torch.Generator().manual_seed(1))
