@@ -24,7 +24,8 @@
  *    pad of the weights at zero) and of 64 for the expert FFN and the offline
  *    search / Hessian tools.
  *  - Arithmetic is IEEE binary32 with one rounding per operation, int32
- *    accumulation, round-half-to-even; results do not depend on launch shape.
+ *    accumulation, round-half-to-even; results do not depend on launch shape
+ *    (the sum over blocks of the 8-bit floating-point linear apart).
  */
 #ifndef HAQ_H
 #define HAQ_H
@@ -180,19 +181,21 @@ int32_t haq_w8a8_linear_asym(const void* x_fp16, int64_t ldx, const float* s, co
  *   activations: one scale for 128 channels of a token.
  * Of either block, a = largest magnitude (NaN apart): scale = a / 448, code = e4m3(v * (448 /
  * a)), binary32, round half to even; a < 2^-100 gives scale 0 and codes 0.  A NaN has a NaN
- * code; an infinity makes its block's scale infinite and its own code NaN: either way every
- * output of the token (or of the 128 channels, in a weight) is NaN.
+ * code; an infinity makes its block's scale infinite and its own code NaN.  So every output
+ * of a token that holds either is NaN; in the weights a NaN makes its output channel NaN, an
+ * infinity the channels of its block.
  *   y[t][n] = round16(act(sum over blocks b of (sx[t][b] * sw[b][n/128]) * p_b)),
  *   p_b = the sum over the block's channels of code products, formed by the matrix
  * instruction: error below 2^-10 of the sum of the products' magnitudes (it sums each eight in
- * whole steps of 2^-13 of the largest).  The sum
- * over blocks is binary32, one fused multiply-add per block; its order goes by the kernel that
- * the sizes choose, so two row counts may differ in the last bits (a call repeated does not).
+ * whole steps of 2^-13 of the largest).  The sum over blocks is binary32, one fused
+ * multiply-add per block; its order goes by the kernel that the sizes choose, so two row
+ * counts may differ in the last bits (a call repeated does not).  The product of two scales is
+ * binary32 too: magnitudes of a token and of a weight block whose product passes 2^145 overflow.
  * ReLU passes NaN on.
  *
  * x and y are binary16 or bfloat16 by dtype (HAQ_F16, HAQ_BF16; both the same), rows
- * [T x K] and [T x N].  K % 16 == 0, K <= 65536, N % 16 == 0, T and N <= 2^24.  T == 0 is a
- * no-op.  y must not overlap an input, but for the rows x of haq_fp8_linear.
+ * [T x K] and [T x N].  K % 16 == 0, K <= 65536, N % 16 == 0, T and N <= 2^24, T * N <=
+ * 2^38.  T == 0 is a no-op.  y must not overlap an input, but for the rows x of haq_fp8_linear.
  *
  * haq_quant_weight_fp8 (offline): w fp32 [K x N] -> wq [K x N] codes, canonical layout,
  *   and w_scale; to be packed with haq_pack_weight like int8 codes (the layout is of bytes).

@@ -8,6 +8,7 @@ namespace haq {
 namespace {
 
 constexpr int MAX_K = 65536, MAX_ROWS = 1 << 24;  // a K-step of 128 channels of all rows or channels keeps its offsets in 32 bits
+constexpr int64_t MAX_OUT = (int64_t)1 << 38;     // a launch has fewer than 2^32 threads
 
 int64_t act_rows(int T) { return round_up(T, 16) + 256; }
 size_t codes_bytes(int T, int K) { return (size_t)round_up(K, 64) * act_rows(T); }
@@ -25,6 +26,7 @@ int check_linear(const char* name, int T, int K, int N, int act, int dtype) {
     if (const int rc = check_rows(name, T, K, dtype)) return rc;
     if (N <= 0) HAQ_FAIL(HAQ_ERR_INVALID_ARG, "%s: N=%d", name, N);
     if (N % 16 != 0 || N > MAX_ROWS) HAQ_FAIL(HAQ_ERR_UNSUPPORTED, "%s: N=%d must be a multiple of 16, at most %d", name, N, MAX_ROWS);
+    if ((int64_t)T * N > MAX_OUT) HAQ_FAIL(HAQ_ERR_UNSUPPORTED, "%s: T=%d N=%d: more than 2^38 outputs", name, T, N);
     if (act != HAQ_ACT_NONE && act != HAQ_ACT_RELU) HAQ_FAIL(HAQ_ERR_UNSUPPORTED, "%s: act=%d", name, act);
     return HAQ_OK;
 }

@@ -273,16 +273,22 @@ def test_norm(T, K, codes):
 @pytest.mark.parametrize("T", [4, 700, 2100])
 @pytest.mark.parametrize("codes", [haq.HAQ_CODES_NONE, haq.HAQ_CODES_I8, haq.HAQ_CODES_E4M3])
 def test_norm_of_extreme_rows(T, codes):
-    """Rows of zeros, of subnormals, of values whose squares overflow binary32, weights of zero and huge ones."""
+    """Rows of zeros, of subnormals, of values whose squares overflow binary32, weights of zero and huge ones; with a residual sums of
+    subnormals and sums that cancel."""
     K = 528
-    x = ref.rows(1, T, K, BF16)
-    x[0] = 0.0
-    x[1] = ref.rows(2, 1, K, BF16)[0] * 2.0 ** -130
-    x[2] = ref.rows(2, 1, K, BF16)[0] * 2.0 ** 100
     weight = torch.randn(K, generator=torch.Generator().manual_seed(3))
     weight[:128], weight[200] = 0.0, 1e20
-    check_norm(x, weight, None, codes, True)
-    check_norm(x, weight, None, codes, True, eps=1e-30)
+    for dtype, small, large in ((BF16, 2.0 ** -130, 2.0 ** 100), (F16, 2.0 ** -20, 2.0 ** 9)):
+        x = ref.rows(1, T, K, dtype)
+        x[0] = 0.0
+        x[1] = (ref.rows(2, 1, K, F16)[0].float() * small).to(dtype)
+        x[2] = (ref.rows(2, 1, K, F16)[0].float() * large).to(dtype)
+        r = ref.rows(6, T, K, dtype)
+        r[1] = (ref.rows(7, 1, K, F16)[0].float() * small).to(dtype)
+        r[3] = -x[3]
+        check_norm(x, weight, None, codes, True)
+        check_norm(x, weight, None, codes, True, eps=1e-30)
+        check_norm(x, weight, r, codes, True)
 
 
 @pytest.mark.parametrize("T", [5, 700, 2100])

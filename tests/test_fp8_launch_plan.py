@@ -63,8 +63,8 @@ def work_groups(kernel, t, M, N, n_cu):
 def test_every_tile_of_a_linear_has_a_work_group(plan):
     rng = random.Random(3)
     sizes = [(int(2 ** rng.uniform(0, 12.5)), 16 * int(2 ** rng.uniform(0, 10)), 16 * int(2 ** rng.uniform(0, 10.5))) for _ in range(1500)]
-    sizes += [(M, K, N) for M in (1, 8, 9, 16, 17, 64, 65) for K in (16, 65536) for N in (16, 65536, MOST_ROWS)]
-    sizes += [(MOST_ROWS, 4096, 4096), (MOST_ROWS, 16, 8192), (200000, 65536, 16), (100000, 4096, 131072)]
+    sizes += [(M, K, N) for M in (1, 8, 9, 16, 17, 64, 65, 8192) for K in (16, 65536) for N in (16, 65536, MOST_ROWS)]
+    sizes += [(MOST_ROWS, 4096, 4096), (MOST_ROWS, 16, 8192), (MOST_ROWS, 65536, 16384), (1 << 19, 16, 1 << 19), (200000, 65536, 16), (100000, 4096, 131072)]
     for n_cu in (256, 64, 304):
         calls = [("c", n_cu, 0, 0)] + [("g", *s) for s in sizes]
         for (M, K, N), launches in zip(sizes, plan(calls)[1:]):

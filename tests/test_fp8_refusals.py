@@ -58,6 +58,12 @@ def test_refused(name, arg, value, code):
     assert haq.lib().haq_last_error().decode().startswith(name + ":")
 
 
+@pytest.mark.parametrize("name", ["haq_gemm_fp8_packed", "haq_fp8_linear"])
+def test_more_outputs_than_a_launch_reaches_are_refused(name):
+    assert call(name, T=1 << 23, N=(1 << 15) + 16, ldy=1 << 16) == UNSUPPORTED
+    assert "2^38" in haq.lib().haq_last_error().decode()
+
+
 def test_norm_without_any_output_is_refused():
     assert call("haq_rmsnorm_quant", codes=0, q=None, scale=None, y=None) == BAD_ARG
 
