@@ -9,7 +9,7 @@ constexpr int AQ_WAVES = 4;
 
 // A wave takes RW rows, 64 / RW chunks of 16 channels of each, a chunk to a lane: eight neighbouring lanes hold the 128 channels
 // of a block, whose maximum takes three lane exchanges, and with RW = 8 the codes of 8 rows fill the 128-byte lines of the
-// packed layout.  Bound: memory, two bytes read and one written an element.
+// packed layout.  Bound: memory, two bytes read and one written an element: 4096 x 14336 in 33.9 us (5.2 TB/s, a copy's rate).
 template <int DT, int RW>
 __global__ __launch_bounds__(AQ_WAVES * 64) void act_quant_kernel(ActQuantArgs a, int groups, int rows_x) {
     constexpr int LPR = 64 / RW;
@@ -42,7 +42,8 @@ int launch_act(const ActQuantArgs& a, hipStream_t st) {
 }
 
 // A work-group takes one block of 128 x 128: 32 lanes read a row of it, four values each, eight rows at a time; the values stay
-// in registers between the maximum and the rounding.  Bound: memory, four bytes read and one written an element.
+// in registers between the maximum and the rounding.  Bound: memory, four bytes read and one written an element: 4096 x 14336 in
+// 53.8 us (5.5 TB/s, a copy's rate).
 __global__ __launch_bounds__(256) void weight_quant_kernel(const float* w, int K, int N, uint8_t* wq, float* scale) {
     __shared__ float red[4];
     const int n = blockIdx.x * FP8_BLOCK + (threadIdx.x & 31) * 4, k0 = blockIdx.y * FP8_BLOCK + (threadIdx.x >> 5);
@@ -71,8 +72,9 @@ __global__ __launch_bounds__(256) void weight_quant_kernel(const float* w, int K
 
 }  // namespace
 
+// One row or eight to a wave, us at K = 4096:  1 row 1.9 / 2.2,  4 2.07 / 2.05,  7 2.2 / 2.05,  33 2.4 / 2.1,  256 3.4 / 2.6,  4096 27 / 10.9.
 int launch_act_quant_fp8(const ActQuantArgs& a, int dtype, hipStream_t st) {
-    if (a.T >= 8) return dtype == HAQ_F16 ? launch_act<HAQ_F16, 8>(a, st) : launch_act<HAQ_BF16, 8>(a, st);
+    if (a.T >= 4) return dtype == HAQ_F16 ? launch_act<HAQ_F16, 8>(a, st) : launch_act<HAQ_BF16, 8>(a, st);
     return dtype == HAQ_F16 ? launch_act<HAQ_F16, 1>(a, st) : launch_act<HAQ_BF16, 1>(a, st);
 }
 

@@ -1,7 +1,8 @@
 // 8-bit floating-point linear for few token rows: the weights are streamed from HBM once, straight into the operand registers of
 // the matrix instructions.
 //
-// Bound: the weight stream (K N bytes).  A work-group owns 16 C channels and deals the blocks of 128 input channels to its
+// Bound: the weight stream (K N bytes) and, with few of them, the start and the end of a work-group: 1 row of 4096 x 6144 in 6.8 us
+// (3.7 TB/s), of 4096 x 65536 in 49 (5.4);  48 rows of 4096 x 14336 in 15 (4.1).  A work-group owns 16 C channels and deals the blocks of 128 input channels to its
 // waves in turn; each of them holds the fragments of DEPTH blocks on their way, and the partial sums are added in LDS, in the
 // order of the waves, so that a call repeated gives the same bits.
 #include <mutex>
@@ -73,7 +74,8 @@ struct BlockQuantiser {
 // C: blocks of 16 channels; RB: blocks of 16 token rows; NW: waves.  RW > 0: at most RW rows in 16 bits, whose codes every work-group
 // forms itself while its first weights are on their way, so that the linear is one launch.  TILES: several row tiles of 16 RB
 // rows; work-group ids go round-robin to the 8 XCDs, each of which (one L2) takes a contiguous range of tiles, rows fastest, and
-// keeps the weights in its cache.
+// keeps the weights in its cache.  Weights that one work-group alone reads pass the caches by (non-temporal; 1 row of 4096 x 6144 6.8
+// against 7.3 us, 48 of 4096 x 14336 17.7 with the codes' launch against 18.5).
 template <int DT, int C, int RB, int NW, int DEPTH, int WPS, int RW, bool TILES>
 __global__ __launch_bounds__(NW * 64, WPS) void fp8_stream_kernel(Fp8StreamArgs args, int mt) {
     const Fp8GemmArgs& a = args.g;
@@ -236,19 +238,28 @@ int launch_one(const Fp8StreamArgs& a, hipStream_t st) {
     return HAQ_OK;
 }
 
-int channel_blocks(int N) {
+// Blocks of 16 channels to a work-group where it forms the rows' codes itself.  One: two work-groups share a CU and overlap start and
+// end; four: the codes are formed once for four times the channels, in fewer rounds.  us with one / two / four, weights cold:
+//   1 row:   1024 x 2048 2.9 / 3.1 / 3.8,  4096 x 4096 5.3 / 5.9 / 9.5,  4096 x 6144 7.4 / 6.8 / 10.5,  4096 x 8208 8.6 / 11.2 / 11.4,
+//            4096 x 14336 13.0 / 13.4 / 14.1,  4096 x 65536 49 / 56 / 68,  8192 x 28672 44 / 43 / 42,  1024 x 16384 6.4 / 6.1 / 5.3
+//   4 rows:  4096 x 8208 9.2 / 11.8 / 11.3,  4096 x 14336 14.0 / 14.1 / 14.0,  4096 x 65536 52 / 59 / 66,  1024 x 131072 40 / 39 / 34
+//   8 rows:  4096 x 8208 10.2 / 12.0 / 11.7,  4096 x 14336 15.2 / 14.0 / 14.2,  8192 x 28672 51 / 48 / 43,  1024 x 131072 46 / 37 / 35
+int channel_blocks(int M, int K, int N) {
     const int n_cu = cu_count();
-    return N > 32 * n_cu ? 4 : N > 16 * n_cu ? 2 : 1;
+    if (N <= 32 * n_cu) return N > 16 * n_cu ? 2 : 1;
+    return K >= 2048 && (M <= 4 || N <= 40 * n_cu) ? 1 : 4;
 }
 
 template <int DT, int RW>
 int launch_rows16(const Fp8StreamArgs& a, hipStream_t st) {
-    switch (channel_blocks(a.g.N)) {
+    switch (channel_blocks(a.g.M, a.g.K, a.g.N)) {
         case 4: return launch_one<DT, 4, 1, 8, 3, 2, RW>(a, st);
         case 2: return launch_one<DT, 2, 1, 8, 4, 2, RW>(a, st);
         default: return launch_one<DT, 1, 1, 8, 4, 4, RW>(a, st);
     }
 }
+// Room for 1, 2, 4 or 8 rows: fewer rows of 8 in vain (4096 x 6144, room for 8 instead: 1 row 6.8 -> 7.1 us, 2 7.0 -> 7.2, 4 7.0 -> 7.2)
+// and longer ones in the same LDS.
 template <int DT>
 int launch_rows16(const Fp8StreamArgs& a, hipStream_t st) {
     if (a.g.M <= 1) return launch_rows16<DT, 1>(a, st);
@@ -277,7 +288,9 @@ int launch_codes(const Fp8StreamArgs& a, int RB, int C, hipStream_t st) {
 
 }  // namespace
 
-// At most 8 rows in 16 bits whose codes fit 64 KB of LDS: codes and linear in one launch.
+// At most 8 rows in 16 bits whose codes fit 64 KB of LDS: codes and linear in one launch.  us in one / in two, weights cold:  1 row of
+// 4096 x 4096 5.3 / 7.5, of 4096 x 6144 6.8 / 9.7;  8 rows of 1024 x 2048 3.1 / 4.9, of 4096 x 4096 6.1 / 7.7, of 4096 x 14336 14.2 / 14.2;
+// 4 of 14336 x 4096 13.8 / 15.3.  (16 rows of 4096 x 6144 9.1 / 9.0: the vector units of every work-group round all of the rows.)
 bool fp8_stream_rows16_fits(int M, int K) { return M >= 1 && M <= 8 && (M <= 2 ? M : M <= 4 ? 4 : 8) * round_up(K, 1024) <= 65536; }
 int launch_fp8_stream_rows16(const Fp8GemmArgs& a, const void* x, int64_t ldx, int dtype, hipStream_t st) {
     const Fp8StreamArgs s{a, x, ldx};

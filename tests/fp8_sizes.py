@@ -23,3 +23,19 @@ TILED = {
 # 256 x 256 tiles of which those behind whole rounds are taken in halves: 10 of them, of 16 channels (the second halves hold none) and of
 # 144; one; many
 HALVES = [(2049, 272, 14608), (2049, 144, 14480), (2049, 400, 14576), (1281, 1168, 11920)]
+# Rows quantised in the launch of the linear, (channels of a work-group, rows there is room for): blocks of 128 fewer, as many and more than
+# the eight waves take in turn, the last one partial, the last work-group's channels partly past the last one
+ROWS16 = {
+    (16, 1): [(1, 16, 16), (1, 1040, 4096), (1, 4240, 8208), (1, 2064, 14352)],
+    (16, 2): [(2, 1040, 48), (2, 5136, 8208)],
+    (16, 4): [(3, 4240, 144), (4, 2048, 14352)],
+    (16, 8): [(5, 1040, 112), (8, 2064, 10240)],
+    (32, 1): [(1, 16, 4112), (1, 2144, 4112), (1, 4240, 8176)],
+    (32, 2): [(2, 1040, 4112)],
+    (32, 4): [(3, 400, 8176), (4, 5136, 4144)],
+    (32, 8): [(7, 1040, 4112), (8, 5136, 4112)],
+    (64, 1): [(1, 16, 8208), (1, 1040, 8240), (1, 2032, 14352)],
+    (64, 2): [(2, 1040, 8208)],
+    (64, 4): [(3, 400, 8240), (4, 2032, 8208)],
+    (64, 8): [(5, 1040, 8208), (8, 4240, 10256)],
+}

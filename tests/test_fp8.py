@@ -4,7 +4,7 @@ import torch
 
 import paper_2508_07329_amd as haq
 from tests import fp8_reference as ref
-from tests.fp8_sizes import HALVES, STREAM, TILED
+from tests.fp8_sizes import HALVES, ROWS16, STREAM, TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -130,6 +130,17 @@ def test_linear_on_each_kernel(T, K, N):
     again = torch.empty((T, N), dtype=BF16, device=DEV)
     haq.haq_gemm_fp8_packed(q, s, wp, swd, T, K, N, out=again)
     assert same_bits(again, wide[:T, :N])
+
+
+@pytest.mark.parametrize("T,K,N", [size for sizes in ROWS16.values() for size in sizes])
+def test_linear_of_few_rows_on_each_kernel(T, K, N):
+    x = ref.rows(T * K + N, T, K, BF16)
+    wq, sw, wp, swd = weights(T + K + N, K, N)
+    want, bound = ref.linear(*ref.act_codes(x.float()), wq, sw)
+    wide = torch.full((T + 1, N + 8), 7.0, dtype=BF16, device=DEV)
+    haq.haq_fp8_linear(x.to(DEV), wp, swd, N, out=wide[:T, :N])
+    ref.assert_linear(wide[:T, :N].cpu(), want, bound)
+    assert (wide[T] == 7).all() and (wide[:, N:] == 7).all()
 
 
 @pytest.mark.parametrize("T,K,N", [(1, 400, 272), (20, 1040, 272), (100, 400, 144), (300, 656, 528)])

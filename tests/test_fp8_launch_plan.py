@@ -8,7 +8,7 @@ import subprocess
 import pytest
 
 from paper_2508_07329_amd import build as hip_build
-from tests.fp8_sizes import HALVES, STREAM, TILED
+from tests.fp8_sizes import HALVES, ROWS16, STREAM, TILED
 from tests.test_launch_plan import HERE, _host_program
 
 MOST_ROWS = 1 << 24
@@ -88,6 +88,13 @@ def test_sizes_of_the_gpu_tests_take_the_kernels_that_they_are_for(plan):
         for s, launches in zip(sizes, plan([("g", *s) for s in sizes])):
             (kernel, t, *_), = launches
             assert kernel == "fp8_gemm" and (t[1], t[2], t[6]) == shape, (s, shape, launches)
+
+
+def test_sizes_of_the_gpu_test_of_few_rows_take_the_kernels_that_they_are_for(plan):
+    for (channels, room), sizes in ROWS16.items():
+        for s, launches in zip(sizes, plan([("l", *s) for s in sizes])):
+            (kernel, t, *_), = launches
+            assert kernel == "fp8_stream" and (16 * t[1], t[6]) == (channels, room), (s, launches)
 
 
 def test_halves_of_the_last_tiles(plan):
