@@ -7,8 +7,8 @@
 //   once --> one fused multiply-add by the block's scale into the binary32 sum.
 // The weights are the first operand, so a lane owns one token (one scale) and four consecutive channels; a wave's channels lie in
 // one block of 128, so their scale is a scalar.
-// Bound: at 256 x 256 the matrix pipes (8192 x 8192 x 8192 in 405 to 418 us, 2.6 to 2.7 PFLOP/s: busy 80 % of the CUs' cycles at the
-// 1.7 GHz that power leaves; LDS 35 %); at 128 x 128 with a tile to a CU the operands' way from L2 (443 x 16000 x 5456 in 66 us: matrix
+// Bound: at 256 x 256 the matrix pipes (8192 x 8192 x 8192 in 405 to 418 us, 2.6 to 2.7 PFLOP/s: busy 80 % of the CUs' cycles, at
+// 1.7 GHz where lighter kernels run at 2.4; LDS 35 %); at 128 x 128 with a tile to a CU the operands' way from L2 (443 x 16000 x 5456 in 66 us: matrix
 // pipes 48 %, 1070 cycles to a K-step, which neither more stages nor more waves shorten).
 #pragma once
 #include "fp8.h"
