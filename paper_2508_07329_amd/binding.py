@@ -463,6 +463,8 @@ def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, res
     given or no codes are asked for, the sum whenever there is a residual; codes HAQ_CODES_I8 (flat int8, scale [T]) or HAQ_CODES_E4M3
     (flat float8_e4m3fn, scale flat [ceil(K/128)][R]) in the packed operand layout."""
     name = "haq_rmsnorm_quant"
+    if not codes and (q_packed is not None or scale is not None):
+        raise HaqError(f"{name}: q_packed and scale are of codes, and codes={codes} asks for none")
     shape, dtype, number, dev, ldx = _first_rows(name, x)
     T, K = shape
     pr = ldr = ps = lds = py = ldy = pq = pscale = 0
@@ -485,8 +487,6 @@ def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, res
         q_type, n_scale = (torch.int8, T) if codes == HAQ_CODES_I8 else (torch.float8_e4m3fn, -(-K // 128) * R)
         q_packed, scale = _codes_buffers(name, -(-K // 64) * 64 * R, q_packed, scale, q_type, n_scale, dev, x)
         pq, pscale = q_packed.data_ptr(), scale.data_ptr()
-    else:
-        q_packed = scale = None
     _check(lib().haq_rmsnorm_quant(x.data_ptr(), ldx, pr, ldr, weight.data_ptr(), eps, number, T, K, ps, lds, py, ldy, codes, pq, pscale,
                                    _raw_stream(dev)))
     return y, sum_out, q_packed, scale

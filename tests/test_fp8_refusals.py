@@ -68,6 +68,12 @@ def test_norm_without_any_output_is_refused():
     assert call("haq_rmsnorm_quant", codes=0, q=None, scale=None, y=None) == BAD_ARG
 
 
+@pytest.mark.parametrize("buffers", [dict(q_packed=torch.zeros(16)), dict(scale=torch.zeros(4))])
+def test_norm_with_buffers_for_codes_that_it_is_not_asked_for_is_refused(buffers):
+    with pytest.raises(haq.HaqError, match="codes"):
+        binding.haq_rmsnorm_quant(torch.zeros(4, 256, dtype=torch.float16), torch.ones(256), 1e-5, **buffers)
+
+
 @pytest.mark.parametrize("name", ["haq_quant_act_fp8_packed", "haq_gemm_fp8_packed", "haq_fp8_linear", "haq_rmsnorm_quant"])
 def test_no_tokens_need_no_buffers(name):
     assert call(name, T=0, **{k: None for k in ORDER[name] if k in POINTERS}) == 0
