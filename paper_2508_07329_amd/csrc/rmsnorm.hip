@@ -6,8 +6,9 @@
 //
 // Bound: memory, 2 to 4 reads and writes of 16 bits and one of 8 an element.  A row is read once: it stays in registers as
 // 16-bit values between the sum of squares, the row maximum (int8) and the rounding.  The squares of 16-bit values are exact
-// in binary64 and so are summed there: the rounded root does not depend on the order of the sum (but for one row in some ten
-// million), and the binary64 units of this chip are as wide as the binary32 ones.
+// in binary64 and so are summed there; the binary64 units of this chip are as wide as the binary32 ones.  The order of the sum goes by
+// K alone, so that a row gives the same bits whatever rows are with it: 16 channels one behind the other; 16 such chunks (256 channels)
+// as a tree over their lanes; then the sums of 256, 16 apart one behind the other and the 16 of those as a tree.
 #include "fp8.h"
 
 namespace haq {
@@ -15,6 +16,7 @@ namespace haq {
 namespace {
 
 constexpr int NORM_WAVES = 16;             // most waves of a work-group
+constexpr int NORM_SUMS = 256;             // sums of 256 channels: K <= 65536 in one row, K <= 16384 in each of four
 constexpr int MAX_GROUPS_X = 1 << 20;      // a grid has fewer than 2^32 threads in a direction
 
 template <int CTRL>
@@ -23,6 +25,14 @@ __device__ __forceinline__ double lanes_f64(double v) {
     const uint32_t lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xf, 0xf, true);
     const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
     return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+
+// Sum over each 16 neighbouring lanes, as a tree.  All lanes must be active.
+__device__ __forceinline__ double sum_of_16_lanes(double v) {
+    v += lanes_f64<HAQ_LANES_XOR1>(v);
+    v += lanes_f64<HAQ_LANES_XOR2>(v);
+    v += lanes_f64<HAQ_LANES_MIRROR8>(v);
+    return v + lanes_f64<HAQ_LANES_MIRROR16>(v);
 }
 
 // h = round16(x + residual), eight values.  In binary16 the sum of two values rounds the same at once or by way of binary32
@@ -49,7 +59,8 @@ __device__ __forceinline__ uint4 add16(const uint4& x, const uint4& r) {
 template <int DT, int RW, int NB, int MAXW, bool I8>
 __global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
     constexpr int LPR = 64 / RW;  // lanes of a wave that share a row
-    __shared__ double sums[NORM_WAVES][RW];
+    constexpr int MOST = NORM_SUMS / RW;
+    __shared__ double sums[RW][MOST];
     __shared__ float maxima[NORM_WAVES][RW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
     int group = (int)(blockIdx.y * gridDim.x + blockIdx.x);
@@ -94,22 +105,19 @@ __global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
             h[b][1] = add16<DT>(h[b][1], s[b][1]);
         }
     }
-    double ss = 0.0;
+    const int nsum = (nchunk + 15) / 16;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         float v[16];
         unpack8<DT>(h[b][0], v);
         unpack8<DT>(h[b][1], v + 8);
+        double ss = 0.0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+        ss = sum_of_16_lanes(ss);
+        const int at = chunk(b) / 16;
+        if (lane % 16 == 0 && at < nsum) sums[rl][at] = ss;
     }
-    ss += lanes_f64<HAQ_LANES_XOR1>(ss);
-    ss += lanes_f64<HAQ_LANES_XOR2>(ss);
-    ss += lanes_f64<HAQ_LANES_MIRROR8>(ss);
-    if (LPR >= 16) ss += lanes_f64<HAQ_LANES_MIRROR16>(ss);
-    if (LPR >= 32) ss += __shfl_xor(ss, 16);
-    if (LPR >= 64) ss += __shfl_xor(ss, 32);
-    if (lane % LPR == 0) sums[wave][rl] = ss;
     __syncthreads();
     // every input has been read: outputs may take the place of x and residual
     if (a.sum && live) {
@@ -123,8 +131,9 @@ __global__ __launch_bounds__(MAXW * 64) void rmsnorm_kernel(NormArgs a) {
             }
         }
     }
-    ss = 0.0;
-    for (int w = 0; w < nw; ++w) ss += sums[w][rl];
+    double ss = lane % 16 < nsum ? sums[rl][lane % 16] : 0.0;
+    for (int at = 16; at < nsum; at += 16) ss += at + lane % 16 < nsum ? sums[rl][at + lane % 16] : 0.0;
+    ss = sum_of_16_lanes(ss);
     const float inv = (float)(1.0 / sqrt(ss / (double)a.K + a.eps));
 
     uint32_t top = 0;  // int8: largest magnitude, as bits, so that infinities and NaN (larger yet) show in it
@@ -212,10 +221,12 @@ int launch_rows(const NormArgs& a, hipStream_t st) {
 
 // One row to a work-group; where there are codes to write, two from 512 rows (two for each CU) on and four from 2048, up to K = 16384.
 // us with one row / two / four:
-//   rows and the sum, no codes:  777 x 2064 5.3 / 5.4 / 5.5,  8192 x 8192 100 / 102 / 110
-//   with e4m3 codes:  1 x 4096 2.8 / 3.2 / 3.9,  64: 3.5 / 3.8 / 4.4;  700 x 2048 4.8 / 4.8 / 5.0,  1024 x 8192 18.6 / 16.4 / 17.7,  1500 x 6144 20.9 / 19.2 / 19.7
-//                     2048 x 4096 18.3 / 16.9 / 16.9,  8000 x 1040 19.5 / 17.6 / 17.5,  8192 x 8192 127 / 117 / 104
-//   with int8 codes:  512 x 8192 11.1 / 11.6 / 14.4,  1024 x 4096 10.8 / 10.6 / 11.6,  4096 x 8192 58.3 / 56.3 / 57.8,  6000 x 2048 31.2 / 28.8 / 27.9
+//   rows and the sum, no codes:  777 x 2064 5.3 / 5.5 / 6.0,  8192 x 8192 100 / 105 / 105
+//   with e4m3 codes and the sum:  1 x 4096 2.8 / 3.1 / 4.2,  64: 3.1 / 3.5 / 4.5;  700 x 2048 4.7 / 4.8 / 5.0,  1024 x 8192 18.5 / 17.0 / 18.6,
+//                     1500 x 6144 20.4 / 18.9 / 20.2,  2048 x 4096 19.0 / 16.9 / 17.2,  8000 x 1040 19.6 / 17.6 / 17.4,  8192 x 8192 129 / 117 / 105
+//   with int8 codes and the sum:  512 x 8192 10.9 / 11.8 / 14.5,  1024 x 4096 10.7 / 10.5 / 12.1,  4096 x 8192 58.9 / 55.7 / 59.0;  with rows too:
+//                     6000 x 2048 31.4 / 29.0 / 28.9;  without residual and sum:  8192 x 8192 61.4 / 56.0 / 58.5
+// (The line from two to four is that of e4m3; int8 gives some 5 % away to it at K = 8192.)
 // Eight rows, whole lines without the help of the L2, gain up to 5 % at 4096 x 4096 and lose as much at 8192 x 8192, where they fill
 // the registers.  (The work-groups of a line's rows on different XCDs: 256 x 4096 4.9 against 4.3, 8192 x 8192 109 against 104.)
 template <int DT>
