@@ -231,7 +231,8 @@ int32_t haq_fp8_linear(const void* x, int64_t ldx, int32_t dtype, const uint8_t*
  * Codes are of v, not of y, so they carry one rounding fewer than y quantised afterwards.
  *
  * x, residual (or NULL), sum, y: 16-bit rows [T x K] of one dtype, row strides in elements (multiples
- * of 8).  weight fp32 [K].  sum (optional, with a residual only): h, the residual stream of the
+ * of 8).  (haq_moe_w8a8_ffn and the int8 linears take binary16 rows only, and haq_gemm_w8a8_packed's y
+ * is binary16 whatever rows its codes come from: with bfloat16 rows, the e4m3 linear or the int8 codes.)  weight fp32 [K].  sum (optional, with a residual only): h, the residual stream of the
  * next layer.  y optional if codes are asked for.  q_packed and scale (both or neither): the packed layout,
  * haq_packed_act_bytes(T, K) bytes, and fp32 [T] or [ceil(K/128)][haq_packed_act_rows(T)]; rows behind the
  * last token are not written.  sum and y may be x or residual themselves (same address and

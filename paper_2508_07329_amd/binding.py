@@ -153,6 +153,13 @@ def _stream_adr():
     return _raw_stream(torch.cuda.current_device())
 
 
+def _f16(name, *rows):
+    """Raises unless all of them are fp16: the library would read (or leave) bits of another type as other numbers."""
+    for t in rows:
+        if t.dtype is not torch.float16:
+            raise HaqError(f"{name}: rows must be fp16, got {t.dtype} {tuple(t.shape)}")
+
+
 def _ws(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
@@ -164,6 +171,7 @@ def haq_version() -> int:
 def haq_smooth_quant_act(x: torch.Tensor, s: torch.Tensor | None):
     """x fp16 [T,K], s fp32 [K] or None -> (q int8 [T,K], row_scale fp32 [T])."""
     T, K = x.shape
+    _f16("haq_smooth_quant_act", x)
     q = torch.empty((T, K), dtype=torch.int8, device=x.device)
     sx = torch.empty((T,), dtype=torch.float32, device=x.device)
     _check(lib().haq_smooth_quant_act(_ptr(x), C.c_int64(x.stride(0)), _ptr(s), T, K, _ptr(q), C.c_int64(K),
@@ -173,6 +181,7 @@ def haq_smooth_quant_act(x: torch.Tensor, s: torch.Tensor | None):
 
 def haq_channel_absmax_f16(x: torch.Tensor, ax: torch.Tensor | None = None) -> torch.Tensor:
     T, K = x.shape
+    _f16("haq_channel_absmax_f16", x)
     if ax is None:
         ax = torch.zeros((K,), dtype=torch.float32, device=x.device)
     _check(lib().haq_channel_absmax_f16(_ptr(x), C.c_int64(x.stride(0)), T, K, _ptr(ax), _stream()))
@@ -233,6 +242,7 @@ def haq_w8a8_linear(x, s, w_packed, w_scale, N: int, act: int = HAQ_ACT_NONE, *,
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
+    _f16("haq_w8a8_linear", x, y)
     if workspace is None:
         workspace = _ws(haq_linear_workspace_bytes(T, K, N), dev)
     acc = q = sx = None
@@ -255,6 +265,7 @@ def haq_w8a8_linear_kn(x, s, wq_kn, w_scale, act: int = HAQ_ACT_NONE, *, out=Non
     T, K = x.shape
     N = wq_kn.shape[1]
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=x.device)
+    _f16("haq_w8a8_linear_kn", x, y)
     if workspace is None:
         workspace = _ws(haq_linear_kn_workspace_bytes(T, K, N), x.device)
     _check(lib().haq_w8a8_linear_kn(_ptr(x), C.c_int64(x.stride(0)), _ptr(s), _ptr(wq_kn), _ptr(w_scale), T, K, N, act, _ptr(y),
@@ -273,6 +284,7 @@ def haq_packed_act_bytes(T: int, K: int) -> int:
 def haq_quant_act_packed(x, s, *, q_packed=None, row_scale=None):
     """x fp16 [T,K] -> (codes in the packed MFMA operand layout (flat int8), row_scale [T])."""
     T, K = x.shape
+    _f16("haq_quant_act_packed", x)
     if q_packed is None:
         q_packed = torch.empty((haq_packed_act_bytes(T, K),), dtype=torch.int8, device=x.device)
     if row_scale is None:
@@ -285,6 +297,9 @@ def haq_quant_act_packed(x, s, *, q_packed=None, row_scale=None):
 def haq_gemm_w8a8_packed(q_packed, row_scale, w_packed, w_scale, T: int, K: int, N: int, act: int = HAQ_ACT_NONE, *,
                          out=None):
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=q_packed.device)
+    _f16("haq_gemm_w8a8_packed", y)
+    if q_packed.dtype is not torch.int8:
+        raise HaqError(f"haq_gemm_w8a8_packed: q_packed must be int8 codes, got {q_packed.dtype}")
     _check(lib().haq_gemm_w8a8_packed(_adr(q_packed), _adr(row_scale), _adr(w_packed), _adr(w_scale), T, K, N, act,
                                       _adr(y), y.stride(0), None, _stream_adr()))
     return y
@@ -502,6 +517,7 @@ def haq_w8a8_ffn(x, s1, w1_packed, w1_scale, F: int, act: int, s2, w2_packed, w2
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
+    _f16("haq_w8a8_ffn", x, y)
     if workspace is None:
         workspace = _ws(haq_ffn_workspace_bytes(T, K, F, N), dev)
     h = torch.empty((T, F), dtype=torch.float16, device=dev) if debug else None
@@ -571,6 +587,7 @@ def haq_moe_w8a8_ffn(x, logits, s_in, experts: list[ExpertWeights], I: int, *, c
     E = len(experts)
     dev = x.device
     y = out if out is not None else torch.empty((T, H), dtype=torch.float16, device=dev)
+    _f16("haq_moe_w8a8_ffn", x, logits, y)
     if workspace is None:
         workspace = _ws(haq_moe_workspace_bytes(T, H, I, E), dev)
     descs = _expert_descs(experts)
@@ -597,6 +614,7 @@ def haq_moe_w8a8_ffn(x, logits, s_in, experts: list[ExpertWeights], I: int, *, c
 def haq_moe_w8a8_ffn_static(x, logits, s_in, experts, I: int, *, out):
     """haq_moe_w8a8_ffn on the library's built-in scratch array: nothing is allocated, so `out` is required."""
     T, H = x.shape
+    _f16("haq_moe_w8a8_ffn_static", x, logits, out)
     E = len(experts)
     descs = _expert_descs(experts)
     _check(lib().haq_moe_w8a8_ffn_static(_adr(x), x.stride(0), _adr(logits), logits.stride(0), _adr(s_in),
@@ -619,6 +637,7 @@ def haq_moe_w8a8_ffn_asym(x, logits, s_in, experts, colsums, I: int, *, out=None
     E = len(experts)
     dev = x.device
     y = out if out is not None else torch.empty((T, H), dtype=torch.float16, device=dev)
+    _f16("haq_moe_w8a8_ffn_asym", x, logits, y)
     if workspace is None:
         workspace = _ws(haq_moe_asym_workspace_bytes(T, H, I, E), dev)
     descs = _expert_descs(experts)
@@ -660,6 +679,7 @@ def haq_cpu_expert_destroy(handle):
 def haq_cpu_expert_ffn(handle, x, s_in, H: int, n_threads: int = 0):
     """x fp16 [n, H] CPU tensor, s_in fp32 [H] CPU tensor or None -> y fp16 [n, H] (CPU)."""
     n = x.shape[0]
+    _f16("haq_cpu_expert_ffn", x)
     y = torch.empty((n, H), dtype=torch.float16)
     _check(lib().haq_cpu_expert_ffn(handle, _ptr(x), C.c_int64(x.stride(0)), _ptr(s_in), n, _ptr(y), C.c_int64(H), n_threads))
     return y
@@ -734,6 +754,7 @@ def haq_smoothing_search_workspace_bytes(T: int, K: int, N: int, n_e: int) -> in
 def haq_reference_matmul_f64(x, w, *, out=None):
     """x fp16 [T,K], w fp32 [K,N] -> X W in binary64 [T,N]."""
     T, K = x.shape
+    _f16("haq_reference_matmul_f64", x)
     N = w.shape[1]
     y = out if out is not None else torch.empty((T, N), dtype=torch.float64, device=x.device)
     _check(lib().haq_reference_matmul_f64(_ptr(x), C.c_int64(x.stride(0)), _ptr(w), T, K, N, _ptr(y), _stream()))
@@ -743,6 +764,7 @@ def haq_reference_matmul_f64(x, w, *, out=None):
 def haq_quant_loss_f64(y, yref):
     """mean (y - yref)^2 over all entries, binary64; returns a 1-element device tensor."""
     T, N = y.shape
+    _f16("haq_quant_loss_f64", y)
     scratch = torch.empty((T,), dtype=torch.float64, device=y.device)
     loss = torch.empty((1,), dtype=torch.float64, device=y.device)
     _check(lib().haq_quant_loss_f64(_ptr(y), C.c_int64(y.stride(0)), _ptr(yref), T, N, _ptr(scratch), _ptr(loss), _stream()))
@@ -752,6 +774,7 @@ def haq_quant_loss_f64(y, yref):
 def haq_smoothing_search(x, w, exponents, use_weight: bool = False, *, workspace=None):
     """Grid search of the smoothing exponent; returns (losses: list[float], best: int, s_best [K] device)."""
     T, K = x.shape
+    _f16("haq_smoothing_search", x)
     N = w.shape[1]
     n_e = len(exponents)
     grid = (C.c_double * n_e)(*[float(e) for e in exponents])
@@ -838,6 +861,7 @@ def haq_inverse_cholesky_workspace_bytes(K: int) -> int:
 
 def haq_hessian_f64(x, s, percdamp: float = 0.01):
     T, K = x.shape
+    _f16("haq_hessian_f64", x)
     H = torch.empty((K, K), dtype=torch.float64, device=x.device)
     _check(lib().haq_hessian_f64(_ptr(x), C.c_int64(x.stride(0)), _ptr(s), T, K, C.c_double(percdamp), _ptr(H), _stream()))
     return H
@@ -854,6 +878,7 @@ def haq_inverse_cholesky_upper_f64(H):
 def haq_hessian_quant_weight(x, w, s, percdamp: float = 0.01, *, workspace=None):
     """x fp16 [T,K] calibration activations, w fp32 [K,N], s [K] or None -> (wq int8 [K,N], w_scale [N])."""
     T, K = x.shape
+    _f16("haq_hessian_quant_weight", x)
     N = w.shape[1]
     wq = torch.empty((K, N), dtype=torch.int8, device=w.device)
     sw = torch.empty((N,), dtype=torch.float32, device=w.device)
@@ -882,6 +907,7 @@ def haq_w8a8_linear_asym(x, s, w_packed, w_scale, w_colsum, N: int, act: int = H
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
+    _f16("haq_w8a8_linear_asym", x, y)
     if workspace is None:
         workspace = _ws(haq_linear_asym_workspace_bytes(T, K, N), dev)
     acc = q = sx = zp = None
@@ -905,6 +931,7 @@ def haq_quantize_layer(x, w, exponents, use_weight: bool = False, percdamp: floa
     """Smoothing search, then Hessian-aware quantisation with the chosen vector.
     Returns (s [K], wq int8 [K,N], w_scale [N], losses: list[float], best: int)."""
     T, K = x.shape
+    _f16("haq_quantize_layer", x)
     N = w.shape[1]
     n_e = len(exponents)
     grid = (C.c_double * n_e)(*[float(e) for e in exponents])
