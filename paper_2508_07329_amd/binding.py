@@ -307,7 +307,7 @@ def haq_gemm_w8a8_packed(q_packed, row_scale, w_packed, w_scale, T: int, K: int,
 
 # ---- 8-bit floating point with block scales, and the norm in front of a linear ------------
 # A serving loop makes these calls, and looking a tensor over takes as long as handing it on: each is looked at once, by
-# _ld_like or _fits, and only what does not pass goes to _rows16 or _flat, which say what is wrong with it.
+# _ld_like, _fits or _is, and only what does not pass goes to _rows16 or _flat, which say what is wrong with it.
 _DTYPES = {torch.float16: HAQ_F16, torch.bfloat16: HAQ_BF16}
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -332,10 +332,11 @@ def _here(name, what, t):
         raise HaqError(f"{name}: {what} is on {t.device}, not on the current GPU")
 
 
-def _flat(name, what, t, dtype, n):
-    """Raises unless t is a contiguous buffer of at least n elements."""
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
-        raise HaqError(f"{name}: {what} must be a contiguous {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)}")
+def _flat(name, what, t, dtype, n, exactly=False):
+    """Raises unless t is a contiguous buffer of at least n elements, or of exactly n."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n or (exactly and t.numel() != n):
+        raise HaqError(f"{name}: {what} must be a contiguous {dtype} tensor of {'' if exactly else 'at least '}{n} elements, "
+                       f"got {t.dtype} {tuple(t.shape)}")
     _here(name, what, t)
 
 
@@ -349,6 +350,11 @@ def _ld_like(t, dtype, shape, dev):
 
 def _fits(t, dtype, n, dev):
     return t.dtype is dtype and t.numel() >= n and t.get_device() == dev and t.is_contiguous()
+
+
+def _is(t, dtype, n, dev):
+    """What a layer holds (weights and their scales) has exactly its size: more would be another layer's, in other strides."""
+    return t.dtype is dtype and t.numel() == n and t.get_device() == dev and t.is_contiguous()
 
 
 def _first_rows(name, x):
@@ -365,16 +371,17 @@ def haq_quant_weight_fp8(w, *, wq=None, w_scale=None):
     name = "haq_quant_weight_fp8"
     K, N = w.shape
     dev, blocks = w.get_device(), (-(-K // 128), -(-N // 128))
-    if dev < 0 or dev != _current_device() or not _fits(w, torch.float32, 0, dev):
+    if dev < 0 or dev != _current_device() or not _is(w, torch.float32, K * N, dev):
         _flat(name, "w", w, torch.float32, K * N)
     if wq is None:
         wq = torch.empty((K, N), dtype=torch.float8_e4m3fn, device=w.device)
-    elif not _fits(wq, torch.float8_e4m3fn, K * N, dev):
-        _flat(name, "wq", wq, torch.float8_e4m3fn, K * N)
+    elif not _is(wq, torch.float8_e4m3fn, K * N, dev) or (wq.shape != w.shape and wq.dim() != 1):
+        _flat(name, "wq", wq, torch.float8_e4m3fn, K * N, True)
+        raise HaqError(f"{name}: wq is {tuple(wq.shape)}, not {(K, N)}")
     if w_scale is None:
         w_scale = torch.empty(blocks, dtype=torch.float32, device=w.device)
-    elif not _fits(w_scale, torch.float32, blocks[0] * blocks[1], dev):
-        _flat(name, "w_scale", w_scale, torch.float32, blocks[0] * blocks[1])
+    elif not _is(w_scale, torch.float32, blocks[0] * blocks[1], dev):
+        _flat(name, "w_scale", w_scale, torch.float32, blocks[0] * blocks[1], True)
     _check(lib().haq_quant_weight_fp8(w.data_ptr(), K, N, wq.data_ptr(), w_scale.data_ptr(), _raw_stream(dev)))
     return wq, w_scale
 
@@ -411,10 +418,10 @@ _BYTES = (torch.int8, torch.uint8, torch.float8_e4m3fn)
 
 def _fp8_weights(name, w_packed, w_scale, K, N):
     n = -(-K // 64) * 64 * (-(-N // 256) * 256)
-    if w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.numel() < n:
+    if w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.numel() != n:
         raise HaqError(f"{name}: w_packed must hold {n} bytes from haq_pack_weight, got {w_packed.dtype} {tuple(w_packed.shape)}")
     _here(name, "w_packed", w_packed)
-    _flat(name, "w_scale", w_scale, torch.float32, -(-K // 128) * -(-N // 128))
+    _flat(name, "w_scale", w_scale, torch.float32, -(-K // 128) * -(-N // 128), True)
 
 
 def _out_rows(name, out, T, N, dtype, dev, device):
@@ -438,8 +445,8 @@ def haq_gemm_fp8_packed(q_packed, block_scale, w_packed, w_scale, T: int, K: int
         _flat(name, "q_packed", q_packed, torch.float8_e4m3fn, n)
         _flat(name, "block_scale", block_scale, torch.float32, n_scale)
     n = -(-K // 64) * 64 * (-(-N // 256) * 256)
-    if (w_packed.numel() < n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
-            or not _fits(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
+    if (w_packed.numel() != n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
+            or not _is(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
         _fp8_weights(name, w_packed, w_scale, K, N)
     dtype = dtype or (torch.float16 if out is None else out.dtype)
     if dtype not in _DTYPES:
@@ -459,8 +466,8 @@ def haq_fp8_linear(x, w_packed, w_scale, N: int, act: int = HAQ_ACT_NONE, *, out
     name = "haq_fp8_linear"
     (T, K), dtype, number, dev, ldx = _first_rows(name, x)
     n = -(-K // 64) * 64 * (-(-N // 256) * 256)
-    if (w_packed.numel() < n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
-            or not _fits(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
+    if (w_packed.numel() != n or w_packed.dtype not in _BYTES or not w_packed.is_contiguous() or w_packed.get_device() != dev
+            or not _is(w_scale, torch.float32, -(-K // 128) * -(-N // 128), dev)):
         _fp8_weights(name, w_packed, w_scale, K, N)
     y, ldy = _out_rows(name, out, T, N, dtype, dev, x.device)
     if workspace is None:
@@ -495,8 +502,8 @@ def haq_rmsnorm_quant(x, weight, eps: float, codes: int = HAQ_CODES_NONE, *, res
         ldy, py = _ld_like(y, dtype, shape, dev), y.data_ptr()
     if ldr < 0 or lds < 0 or ldy < 0:
         _rows16(name, x=x, residual=residual, sum_out=sum_out, y=y)
-    if not _fits(weight, torch.float32, K, dev):
-        _flat(name, "weight", weight, torch.float32, K)
+    if not _is(weight, torch.float32, K, dev):
+        _flat(name, "weight", weight, torch.float32, K, True)
     if codes:
         R = -(-T // 16) * 16 + 256
         q_type, n_scale = (torch.int8, T) if codes == HAQ_CODES_I8 else (torch.float8_e4m3fn, -(-K // 128) * R)
