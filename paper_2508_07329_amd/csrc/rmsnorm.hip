@@ -215,8 +215,10 @@ int launch_rows(const NormArgs& a, hipStream_t st) {
     const int need = cdiv(a.K / 16, 64 / RW);  // wave-wide pieces of RW rows
     if (need <= 8) return launch_one<DT, RW, 1, 8>(a, need, st);
     if (need <= 16) return launch_one<DT, RW, 2, 8>(a, cdiv(need, 2), st);
-    if (need <= 32) return launch_one<DT, RW, 4, 8>(a, cdiv(need, 4), st);
-    return launch_one<DT, RW, 4, 16>(a, cdiv(need, 4), st);
+    if constexpr (RW == 4) {  // two rows of K <= 16384 never need more
+        if (need > 32) return launch_one<DT, RW, 4, 16>(a, cdiv(need, 4), st);
+    }
+    return launch_one<DT, RW, 4, 8>(a, cdiv(need, 4), st);
 }
 
 // One row to a work-group; where there are codes to write, two from 512 rows (two for each CU) on and four from 2048, up to K = 16384.
