@@ -1,5 +1,5 @@
-"""Every kernel that is built for the 8-bit floating-point calls and the norm is launched by some call: the host code over the recording
-stand-in for the HIP runtime."""
+"""Every kernel that is built for the 8-bit floating-point calls and the norm is launched by some call, and by some size of the GPU tests: the
+host code over the recording stand-in for the HIP runtime."""
 import os
 import random
 import re
@@ -45,3 +45,16 @@ def test_every_kernel_is_launched_by_some_call(program):
     kernels = built(program)
     assert len(kernels) > 40
     assert kernels == launched(program, calls)
+
+
+def test_every_kernel_is_run_by_a_gpu_test(program):
+    """In both types: these tests go over the types themselves."""
+    from tests import test_fp8, test_fp8_each_kernel
+    of = lambda test, names: next(mark.args[1] for mark in test.pytestmark if mark.name == "parametrize" and mark.args[0] == names)
+    calls = [("w", *size, 0) for size in of(test_fp8.test_weight_codes, "K,N")]
+    calls += [("q", *size, 0) for size in of(test_fp8.test_activation_codes, "T,K")]
+    for test in (test_fp8.test_norm, test_fp8_each_kernel.test_norm_between):
+        calls += [("n", *size, codes) for size in of(test, "T,K") for codes in of(test, "codes")]
+    calls += [("g", *size) for size in of(test_fp8_each_kernel.test_on_codes, "T,K,N")]
+    calls += [("l", *size) for size in of(test_fp8_each_kernel.test_on_few_rows, "T,K,N")]
+    assert built(program) == launched(program, calls)
