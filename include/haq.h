@@ -190,7 +190,8 @@ int32_t haq_w8a8_linear_asym(const void* x_fp16, int64_t ldx, const float* s, co
  * whole steps of 2^-13 of the largest).  The sum over blocks is binary32, one fused
  * multiply-add per block; its order goes by the kernel that the sizes choose, so two row
  * counts may differ in the last bits (a call repeated does not).  The product of two scales is
- * binary32 too: magnitudes of a token and of a weight block whose product passes 2^145 overflow.
+ * binary32 too: magnitudes of a token and of a weight block whose product passes 2^145 overflow, and
+ * below 2^-108 it is subnormal, an error of up to 2^-150 |p_b| (less than 2^-125), from 2^-133 down zero.
  * ReLU passes NaN on.
  *
  * x and y are binary16 or bfloat16 by dtype (HAQ_F16, HAQ_BF16; both the same), rows
