@@ -153,10 +153,14 @@ def _stream_adr():
     return _raw_stream(torch.cuda.current_device())
 
 
+_F16 = torch.float16
+
+
 def _f16(name, *rows):
-    """Raises unless all of them are fp16: the library would read (or leave) bits of another type as other numbers."""
+    """Raises unless all of them are fp16: the library would read (or leave) bits of another type as other numbers.  (The calls of a
+    serving loop look at the types themselves first: half the time of this call.)"""
     for t in rows:
-        if t.dtype is not torch.float16:
+        if t.dtype is not _F16:
             raise HaqError(f"{name}: rows must be fp16, got {t.dtype} {tuple(t.shape)}")
 
 
@@ -242,7 +246,8 @@ def haq_w8a8_linear(x, s, w_packed, w_scale, N: int, act: int = HAQ_ACT_NONE, *,
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
-    _f16("haq_w8a8_linear", x, y)
+    if not (x.dtype is y.dtype is _F16):
+        _f16("haq_w8a8_linear", x, y)
     if workspace is None:
         workspace = _ws(haq_linear_workspace_bytes(T, K, N), dev)
     acc = q = sx = None
@@ -284,7 +289,8 @@ def haq_packed_act_bytes(T: int, K: int) -> int:
 def haq_quant_act_packed(x, s, *, q_packed=None, row_scale=None):
     """x fp16 [T,K] -> (codes in the packed MFMA operand layout (flat int8), row_scale [T])."""
     T, K = x.shape
-    _f16("haq_quant_act_packed", x)
+    if x.dtype is not _F16:
+        _f16("haq_quant_act_packed", x)
     if q_packed is None:
         q_packed = torch.empty((haq_packed_act_bytes(T, K),), dtype=torch.int8, device=x.device)
     if row_scale is None:
@@ -297,7 +303,8 @@ def haq_quant_act_packed(x, s, *, q_packed=None, row_scale=None):
 def haq_gemm_w8a8_packed(q_packed, row_scale, w_packed, w_scale, T: int, K: int, N: int, act: int = HAQ_ACT_NONE, *,
                          out=None):
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=q_packed.device)
-    _f16("haq_gemm_w8a8_packed", y)
+    if y.dtype is not _F16:
+        _f16("haq_gemm_w8a8_packed", y)
     if q_packed.dtype is not torch.int8:
         raise HaqError(f"haq_gemm_w8a8_packed: q_packed must be int8 codes, got {q_packed.dtype}")
     _check(lib().haq_gemm_w8a8_packed(_adr(q_packed), _adr(row_scale), _adr(w_packed), _adr(w_scale), T, K, N, act,
@@ -524,7 +531,8 @@ def haq_w8a8_ffn(x, s1, w1_packed, w1_scale, F: int, act: int, s2, w2_packed, w2
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
-    _f16("haq_w8a8_ffn", x, y)
+    if not (x.dtype is y.dtype is _F16):
+        _f16("haq_w8a8_ffn", x, y)
     if workspace is None:
         workspace = _ws(haq_ffn_workspace_bytes(T, K, F, N), dev)
     h = torch.empty((T, F), dtype=torch.float16, device=dev) if debug else None
@@ -594,7 +602,8 @@ def haq_moe_w8a8_ffn(x, logits, s_in, experts: list[ExpertWeights], I: int, *, c
     E = len(experts)
     dev = x.device
     y = out if out is not None else torch.empty((T, H), dtype=torch.float16, device=dev)
-    _f16("haq_moe_w8a8_ffn", x, logits, y)
+    if not (x.dtype is logits.dtype is y.dtype is _F16):
+        _f16("haq_moe_w8a8_ffn", x, logits, y)
     if workspace is None:
         workspace = _ws(haq_moe_workspace_bytes(T, H, I, E), dev)
     descs = _expert_descs(experts)
@@ -621,7 +630,8 @@ def haq_moe_w8a8_ffn(x, logits, s_in, experts: list[ExpertWeights], I: int, *, c
 def haq_moe_w8a8_ffn_static(x, logits, s_in, experts, I: int, *, out):
     """haq_moe_w8a8_ffn on the library's built-in scratch array: nothing is allocated, so `out` is required."""
     T, H = x.shape
-    _f16("haq_moe_w8a8_ffn_static", x, logits, out)
+    if not (x.dtype is logits.dtype is out.dtype is _F16):
+        _f16("haq_moe_w8a8_ffn_static", x, logits, out)
     E = len(experts)
     descs = _expert_descs(experts)
     _check(lib().haq_moe_w8a8_ffn_static(_adr(x), x.stride(0), _adr(logits), logits.stride(0), _adr(s_in),
@@ -644,7 +654,8 @@ def haq_moe_w8a8_ffn_asym(x, logits, s_in, experts, colsums, I: int, *, out=None
     E = len(experts)
     dev = x.device
     y = out if out is not None else torch.empty((T, H), dtype=torch.float16, device=dev)
-    _f16("haq_moe_w8a8_ffn_asym", x, logits, y)
+    if not (x.dtype is logits.dtype is y.dtype is _F16):
+        _f16("haq_moe_w8a8_ffn_asym", x, logits, y)
     if workspace is None:
         workspace = _ws(haq_moe_asym_workspace_bytes(T, H, I, E), dev)
     descs = _expert_descs(experts)
@@ -914,7 +925,8 @@ def haq_w8a8_linear_asym(x, s, w_packed, w_scale, w_colsum, N: int, act: int = H
     T, K = x.shape
     dev = x.device
     y = out if out is not None else torch.empty((T, N), dtype=torch.float16, device=dev)
-    _f16("haq_w8a8_linear_asym", x, y)
+    if not (x.dtype is y.dtype is _F16):
+        _f16("haq_w8a8_linear_asym", x, y)
     if workspace is None:
         workspace = _ws(haq_linear_asym_workspace_bytes(T, K, N), dev)
     acc = q = sx = zp = None
