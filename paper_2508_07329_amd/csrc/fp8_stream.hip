@@ -2,9 +2,13 @@
 // the matrix instructions.
 //
 // Bound: the weight stream (K N bytes) and, with few of them, the start and the end of a work-group: 1 row of 4096 x 6144 in 6.8 us
-// (3.7 TB/s), of 4096 x 65536 in 49 (5.4);  48 rows of 4096 x 14336 in 15 (4.1).  A work-group owns 16 C channels and deals the blocks of 128 input channels to its
-// waves in turn; each of them holds the fragments of DEPTH blocks on their way, and the partial sums are added in LDS, in the
+// (3.7 TB/s), of 4096 x 65536 in 49 (5.5);  48 rows of 4096 x 14336 in 15 (3.9).  A work-group owns 16 C channels and deals the blocks of 128 input channels to its
+// waves in turn; each of them has room for the fragments of DEPTH blocks on their way, and the partial sums are added in LDS, in the
 // order of the waves, so that a call repeated gives the same bits.
+// Where the rows come as codes the ring is not kept full: the compiler mixes the loads of the first DEPTH blocks, and the wait at the head
+// of the loop, which serves its entry and every later trip, holds for the mixed order.  Loads still on their way at a trip's first
+// product, and what the order of the blocks would allow: 16 x 16 6 of 20 (15), 16 x 32 4 of 21 (14), 16 x 64 6 of 44 (33), 32 x 32 12 of 40
+// (30), 64 x 32 16 of 48 (32), 64 x 64 8 of 40 (20); 32 x 64 and the rows in 16 bits, whose fetch stands between barriers, keep theirs.
 #include <mutex>
 
 #include "fp8_gemm_kernel.h"
@@ -244,6 +248,7 @@ int launch_one(const Fp8StreamArgs& a, hipStream_t st) {
 //            4096 x 14336 13.0 / 13.4 / 14.1,  4096 x 65536 49 / 56 / 68,  8192 x 28672 44 / 43 / 42,  1024 x 16384 6.4 / 6.1 / 5.3
 //   4 rows:  4096 x 8208 9.2 / 11.8 / 11.3,  4096 x 14336 14.0 / 14.1 / 14.0,  4096 x 65536 52 / 59 / 66,  1024 x 131072 40 / 39 / 34
 //   8 rows:  4096 x 8208 10.2 / 12.0 / 11.7,  4096 x 14336 15.2 / 14.0 / 14.2,  8192 x 28672 51 / 48 / 43,  1024 x 131072 46 / 37 / 35
+// (One row of long K on wide layers lies close: at 8192 x 28672 the line gives 2 us of 44 away, at 4096 x 65536 it gains 19 of 68.)
 int channel_blocks(int M, int K, int N) {
     const int n_cu = cu_count();
     if (N <= 32 * n_cu) return N > 16 * n_cu ? 2 : 1;
