@@ -227,7 +227,8 @@ int32_t haq_fp8_linear(const void* x, int64_t ldx, int32_t dtype, const uint8_t*
  * codes:
  *   HAQ_CODES_I8: a = max_k |v|, scale = a / 127, q = rne(v / scale): the operand of
  *     haq_gemm_w8a8_packed.  For a smoothed layer pass weight_k / s_k.  a < 2^-100 gives scale 0,
- *     codes 0; with an infinity or NaN in the row scale is not finite either, codes 0 (every output NaN).
+ *     codes 0; with an infinity or NaN in the row scale is not finite either, codes 0 (every output of
+ *     haq_gemm_w8a8_packed NaN, but zero behind its ReLU, which takes the larger of a NaN and 0 to be 0).
  *   HAQ_CODES_E4M3: as haq_quant_act_fp8_packed, on v: the operand of haq_gemm_fp8_packed.
  * Codes are of v, not of y, so they carry one rounding fewer than y quantised afterwards.
  *
