@@ -27,3 +27,18 @@ def test_small_scales(T, K, N):
     ref.assert_linear(y.cpu(), want, bound)
     normal = product > 2.0 ** -120  # where nothing is lost, outputs are not all zero
     assert not bool(normal.any()) or bool((y.cpu()[normal] != 0).any(dim=1).all())
+
+
+@pytest.mark.parametrize("T,K,N", [(3, 400, 400), (20, 1040, 400), (60, 400, 400), (200, 400, 400), (65, 3216, 8208), (513, 336, 14576)])
+def test_an_infinite_weight_takes_the_channels_of_its_block(T, K, N):
+    """In the last block of channels and in the one before it."""
+    x = ref.rows(T, T, K, torch.float16)
+    x[1, K - 16:] = 0.0
+    x[2, (K - 1) // 128 * 128:] = 0.0  # a scale of zero meets the infinite one
+    for k in (K - 1, (K - 1) // 128 * 128 - 1):
+        w = torch.randn(K, N, generator=torch.Generator().manual_seed(1)) * 0.02
+        w[k, 200] = -float("inf")
+        wq, sw = haq.haq_quant_weight_fp8(w.to(DEV))
+        assert sw.isinf().nonzero().tolist() == [[k // 128, 1]]
+        y = haq.haq_fp8_linear(x.to(DEV), haq.haq_pack_weight(wq), sw, N)
+        assert bool(y[:, 128:256].isnan().all()) and not bool(y[:, :128].isnan().any()) and not bool(y[:, 256:].isnan().any())
